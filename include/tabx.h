@@ -59,7 +59,7 @@ enum TabxError {
     TABX_ERR_SHAPE = -2,     /* sizes out of range (N, zones, grid, negative E ...) */
     TABX_ERR_ALIGN = -3,     /* a pointer is not aligned as required                */
     TABX_ERR_LAUNCH = -4,    /* the HIP runtime refused the launch                  */
-    TABX_ERR_PARAM = -5      /* a physics constant is not finite / not positive     */
+    TABX_ERR_PARAM = -5      /* a physics constant or a setting is out of its range */
 };
 
 /* Physics and shape constants (App. A "Environment Parameters": the physics
@@ -379,6 +379,132 @@ typedef struct TabxRowForm {
     int32_t streams_global_state;    /* 1: the global state goes past the caches                   */
 } TabxRowForm;
 int tabx_row_form(const TabxParams *params, int call, TabxRowForm *form);
+
+/* ---------------------------------------------------------------------------------------------
+ * The learner's side of the tick: its first operator on the rows a call writes (layer norm), the
+ * actions and levels it answers with (draws from scores), and the way back of a training step.
+ * These calls work on `rows` rows of the caller's own arrays, whatever they stand for: the E * N
+ * units of a batch, some ticks of it, a part, the E envs.  Stream rules and errors are those of the
+ * other calls; the device that owns `stream` and the arrays has to be the current one.  rows == 0
+ * is a no-op that needs no arrays.  rows may not exceed 2^40, nor rows times a stride 2^62
+ * (TABX_ERR_SHAPE).  Outputs must not overlap inputs or each other, except where it is said.
+ * ------------------------------------------------------------------------------------------- */
+
+/* Element types of the learner's arrays. */
+enum TabxType { TABX_F32 = 0, TABX_BF16 = 1, TABX_F16 = 2 };
+
+/* Rows of a two-dimensional device array: element j of row r is data[r * stride + j], so the rows
+ * may be some columns of a wider array.  `data` is aligned to its element only (TABX_ERR_ALIGN).
+ * stride >= the width of the rows (TABX_ERR_SHAPE). */
+typedef struct TabxRows {
+    void    *data;
+    int64_t  stride;           /* elements between two rows                                */
+    int32_t  type;             /* TabxType                                                 */
+} TabxRows;
+
+#define TABX_NORM_MAX_WIDTH 16384     /* widest row of the layer norm                      */
+#define TABX_SAMPLE_MAX_LEVELS 16384  /* most levels tabx_sample_levels chooses between    */
+
+/* Layer norm of every row with row_mask[r] != 0 (NULL: all; pass `controlled` to leave out the
+ * units that do not learn):
+ *   mean = sum_j x_j / width, rstd = 1 / sqrt(sum_j (x_j - mean)^2 / width + eps),
+ *   y_j = (x_j - mean) * rstd * weight_j + bias_j,
+ * in 32 bits, y rounded once to its type.  weight / bias: device [width] f32, NULL = all one / all
+ * zero.  mean / rstd: device [rows] f32, both or neither; a backward pass needs them.
+ * eps >= 0 and finite (TABX_ERR_PARAM); 1 <= width <= TABX_NORM_MAX_WIDTH (TABX_ERR_SHAPE).  Rows
+ * that are masked out are neither read nor written, in any output.  y may be x itself (same data,
+ * stride and type). */
+int tabx_layer_norm(int64_t rows, int32_t width, const TabxRows *x, const uint8_t *row_mask,
+                    const float *weight, const float *bias, float eps, const TabxRows *y,
+                    float *mean, float *rstd, void *stream);
+
+/* Its gradients, from the gradient of y and the mean and rstd of the forward call:
+ *   h_j = (x_j - mean) * rstd, g_j = grad_y_j * weight_j,
+ *   grad_x_j = rstd * (g_j - sum_j g_j / width - h_j * sum_j (g_j h_j) / width),
+ *   grad_weight_j = sum over rows of grad_y_j h_j, grad_bias_j = sum over rows of grad_y_j.
+ * Rows that are masked out are not read and add nothing; their grad_x is zero.  grad_x (NULL:
+ * not wanted, as for an observation) may be grad_y itself.  grad_weight / grad_bias: device
+ * [width] f32, overwritten (with zeros if there are no rows), each may be NULL.  The sums are always taken in the same order: equal
+ * calls give equal bits.  `workspace`: device memory, 16-byte aligned, of at least
+ * tabx_layer_norm_workspace(rows, width) bytes (TABX_ERR_SHAPE if workspace_bytes is less), needed
+ * only for grad_weight and grad_bias.  Its contents need no preparation; it belongs to the call
+ * until the enqueued work has finished, so calls (and replays of captured graphs) that may run at
+ * the same time need one each. */
+int tabx_layer_norm_backward(int64_t rows, int32_t width, const TabxRows *x,
+                             const uint8_t *row_mask, const float *weight, const float *mean,
+                             const float *rstd, const TabxRows *grad_y, const TabxRows *grad_x,
+                             float *grad_weight, float *grad_bias, void *workspace,
+                             int64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace of a tabx_layer_norm_backward call; host only.  Negative TabxError. */
+int64_t tabx_layer_norm_workspace(int64_t rows, int32_t width);
+
+/* How a choice is drawn from scores (logits) l_i.  The choices that are allowed and whose score is
+ * above -infinity (NaN counts as -infinity) have the weights w_i = exp((l_i - max l) / temperature).
+ * Among them are kept
+ *   - the top_k largest, if top_k >= 1 (0: all);
+ *   - of those, in falling order, each one whose predecessors' weights sum to less than top_p
+ *     times the sum of all of them (top_p = 1: all);
+ *   - of those, the ones with w_i >= min_p (the largest weight is 1);
+ * equal scores are in order of their index.  The draw lays the kept weights side by side in order
+ * of index and takes the one into which uniform * (their sum) points: the first whose running sum
+ * exceeds it.  The weights and sums have at least 48 bits after the point.  temperature = 0 takes
+ * the largest score, the lowest index among equals.  An infinite largest score shares the draw
+ * among those equal to it.
+ * temperature 0 or in [1e-30, 1e30], top_k >= 0, 0 < top_p <= 1, 0 <= min_p <= 1 (TABX_ERR_PARAM). */
+typedef struct TabxSampling {
+    float    temperature;
+    int32_t  top_k;
+    float    top_p;
+    float    min_p;
+} TabxSampling;
+
+/* Draws actions[r] for every row (unit) with controlled[r] != 0 (NULL: all) from its
+ * TABX_NUM_ACTIONS logits; other entries of `actions` and `log_prob` are not written (so the same
+ * array takes the scripted units' actions too).  action_mask [rows] u8 as the observing calls
+ * write it: where it is 0 the combat action is not allowed (NULL: allowed everywhere).
+ * uniform [rows] f32: the random numbers, in [0, 1) (below 0 and NaN are taken as 0, from 1 on as
+ * the largest below 1).  log_prob [rows] f32 (NULL: not wanted): the logarithm of the probability
+ * of the action among ALL allowed ones at this temperature (0 at temperature 0), as
+ * tabx_action_log_prob gives it.  A row without any allowed choice idles: TABX_ACT_NOOP,
+ * log_prob 0. */
+int tabx_sample_actions(int64_t rows, const TabxRows *logits, const uint8_t *action_mask,
+                        const uint8_t *controlled, const TabxSampling *sampling,
+                        const float *uniform, uint8_t *actions, float *log_prob, void *stream);
+
+/* Draws next_level[e] (int32, TabxState.next_level) for every env with env_mask[e] != 0 (NULL:
+ * all), by the same rules, from the scores of num_levels levels: a curriculum instead of the
+ * uniform draw.  scores: one row for all envs (stride 0), or a row per env (stride >= num_levels).
+ * level_mask [num_levels] u8: where it is 0 a level is not drawn by any env (NULL: all may be).
+ * An env without any allowed level keeps the next_level it has.
+ * 1 <= num_levels <= TABX_SAMPLE_MAX_LEVELS; envs <= 2^30 (TABX_ERR_SHAPE). */
+int tabx_sample_levels(int64_t envs, int32_t num_levels, const TabxRows *scores,
+                       const uint8_t *level_mask, const uint8_t *env_mask,
+                       const TabxSampling *sampling, const float *uniform, int32_t *next_level,
+                       void *stream);
+
+/* Of the distribution p_i = w_i / sum w over all allowed actions (weights as in TabxSampling,
+ * nothing else left out), for every row with controlled[r] != 0 (NULL: all):
+ *   log_prob[r] = log p_a of the action a = actions[r] (an id >= TABX_NUM_ACTIONS acts as
+ *     TABX_ACT_NOOP); -infinity if a is not allowed;
+ *   entropy[r] = -sum_i p_i log p_i (entropy NULL: not wanted).
+ * [rows] f32; other rows are not written; a row without any allowed choice has 0 in both.
+ * 1e-30 <= temperature <= 1e30 (TABX_ERR_PARAM). */
+int tabx_action_log_prob(int64_t rows, const TabxRows *logits, const uint8_t *action_mask,
+                         const uint8_t *controlled, const uint8_t *actions, float temperature,
+                         float *log_prob, float *entropy, void *stream);
+
+/* The gradient of both with respect to the logits:
+ *   grad_logits_i = (grad_log_prob (1[i = a] - p_i) - grad_entropy p_i (log p_i + entropy)) / temperature
+ * for the allowed choices, zero for the others and for rows that are not controlled (these are
+ * written: the gradient of logits that were not used).  grad_log_prob / grad_entropy [rows] f32,
+ * each may be NULL (zero), not both; a log_prob of -infinity passes nothing back.  The elements of
+ * grad_logits between its rows are not written.  grad_logits may be `logits` itself. */
+int tabx_action_log_prob_backward(int64_t rows, const TabxRows *logits, const uint8_t *action_mask,
+                                  const uint8_t *controlled, const uint8_t *actions,
+                                  float temperature, const float *grad_log_prob,
+                                  const float *grad_entropy, const TabxRows *grad_logits,
+                                  void *stream);
 
 const char *tabx_strerror(int code);
 

@@ -26,7 +26,9 @@ STATE_FLOAT = ("x", "y", "vx", "vy", "theta", "hp", "cd", "reveal", "cur_speed")
 EXPORTS = ("tabx_obs_dim", "tabx_num_actions", "tabx_reset", "tabx_step", "tabx_observe",
            "tabx_step_observe", "tabx_global_state", "tabx_heuristic_actions",
            "tabx_policy_step_observe", "tabx_scripted_step_observe", "tabx_part", "tabx_launch_info",
-           "tabx_row_form", "tabx_strerror")
+           "tabx_row_form", "tabx_layer_norm", "tabx_layer_norm_backward",
+           "tabx_layer_norm_workspace", "tabx_sample_actions", "tabx_sample_levels",
+           "tabx_action_log_prob", "tabx_action_log_prob_backward", "tabx_strerror")
 
 _I8 = C.POINTER(C.c_int8)
 _I32 = C.POINTER(C.c_int32)
@@ -78,6 +80,20 @@ class TabxPolicyMemory(C.Structure):
     _fields_ = [("mem_x", _F), ("mem_y", _F), ("mem_valid", _U8), ("next_action", _U8)]
 
 
+class TabxRows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_int64), ("type", C.c_int32)]
+
+
+class TabxSampling(C.Structure):
+    """How a choice is drawn: temperature (0: the largest score), top_k (0: all), top_p (1: all),
+    min_p (0: all)."""
+    _fields_ = [("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float),
+                ("min_p", C.c_float)]
+
+    def __init__(self, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+        super().__init__(temperature, top_k, top_p, min_p)
+
+
 def load_library(path: str = LIB_PATH) -> C.CDLL:
     if not os.path.exists(path):
         raise ImportError(
@@ -99,8 +115,17 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.tabx_scripted_step_observe.argtypes = lib.tabx_policy_step_observe.argtypes
     lib.tabx_strerror.argtypes = [C.c_int]
     lib.tabx_strerror.restype = C.c_char_p
+    R, W, I64, I32, F32 = C.POINTER(TabxRows), C.POINTER(TabxSampling), C.c_int64, C.c_int32, C.c_float
+    lib.tabx_layer_norm.argtypes = [I64, I32, R, V, V, V, F32, R, V, V, V]
+    lib.tabx_layer_norm_backward.argtypes = [I64, I32, R, V, V, V, V, R, R, V, V, V, I64, V]
+    lib.tabx_layer_norm_workspace.argtypes = [I64, I32]
+    lib.tabx_sample_actions.argtypes = [I64, R, V, V, W, V, V, V, V]
+    lib.tabx_sample_levels.argtypes = [I64, I32, R, V, V, W, V, V, V]
+    lib.tabx_action_log_prob.argtypes = [I64, R, V, V, V, F32, V, V, V]
+    lib.tabx_action_log_prob_backward.argtypes = [I64, R, V, V, V, F32, V, V, R, V]
     for name in EXPORTS[:-1]:
         getattr(lib, name).restype = C.c_int
+    lib.tabx_layer_norm_workspace.restype = I64
     return lib
 
 
@@ -235,6 +260,203 @@ def tabx_scripted_step_observe(params, scenario, state, policy, memory, controll
                                            _ptr(vis_mask), _ptr(action_mask),
                                            _stream_ptr(stream)),
            "tabx_scripted_step_observe")
+
+
+# --- the learner's side of the tick: tensors of its own, checked before their addresses are taken ---
+
+TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+class _Call:
+    """The arguments of one call as the library takes them.  Every tensor has to be on one GPU."""
+
+    def __init__(self, what: str):
+        self.what, self.device, self.host = what, None, None
+
+    def refuse(self, why: str):
+        raise TabxError(f"{self.what}: {why}")
+
+    def _place(self, t, name):
+        d = t.device
+        if self.device is None:
+            self.device = d
+        elif d != self.device:
+            self.refuse(f"{name} is on {d}, not on {self.device}")
+        if d.type != "cuda":
+            self.host = name               # (refused last, after what is wrong with its shape)
+
+    def rows(self, t, name, width=0):
+        """(TabxRows, rows, width) of a tensor [..., width] whose rows lie at equal distances."""
+        code = TYPES.get(t.dtype)
+        if code is None:
+            self.refuse(f"{name} is {t.dtype}, not one of float32, bfloat16, float16")
+        n = t.dim()
+        if n < 1:
+            self.refuse(f"{name} has no dimensions")
+        shape, stride = t.shape, t.stride()
+        wide = shape[-1]
+        if width and wide != width:
+            self.refuse(f"{name} has rows of {wide} elements, not {width}")
+        if wide > 1 and stride[-1] != 1:
+            self.refuse(f"the elements of a row of {name} are not next to each other")
+        count, apart = 1, 0
+        for k in range(n - 2, -1, -1):     # the leading dimensions have to be one run of rows
+            if shape[k] == 1:
+                continue
+            if apart == 0:
+                apart = stride[k]
+            elif stride[k] != apart * count:
+                self.refuse(f"the rows of {name} do not lie at equal distances")
+            count *= shape[k]
+        if count > 1 and apart < wide:
+            self.refuse(f"the rows of {name} overlap")
+        self._place(t, name)
+        return TabxRows(t.data_ptr(), max(apart, wide), code), count, wide
+
+    def array(self, t, name, count, dtype):
+        """Address of a contiguous tensor of `count` elements, None for None."""
+        if t is None:
+            return None
+        if t.dtype is not dtype:
+            self.refuse(f"{name} is {t.dtype}, not {dtype}")
+        if t.numel() != count:
+            self.refuse(f"{name} has {t.numel()} elements, not {count}")
+        if not t.is_contiguous():
+            self.refuse(f"{name} is not contiguous")
+        self._place(t, name)
+        return t.data_ptr()
+
+    def needed(self, t, name, count, dtype):
+        if t is None:
+            self.refuse(f"{name} is needed")
+        return self.array(t, name, count, dtype)
+
+    def make(self, function, stream, *args):
+        if self.host is not None:
+            self.refuse(f"{self.host} is not on a GPU")
+        here = torch.cuda.current_device()
+        if stream is None:
+            stream = torch.cuda.current_stream(self.device)
+        elif stream.device != self.device:
+            self.refuse(f"the stream is on {stream.device}, the tensors on {self.device}")
+        if self.device.index == here:
+            rc = function(*args, stream.cuda_stream)
+        else:
+            with torch.cuda.device(self.device):
+                rc = function(*args, stream.cuda_stream)
+        if rc != 0:
+            _check(rc, self.what)
+
+
+def tabx_layer_norm(x, weight, bias, eps, y, mean=None, rstd=None, row_mask=None, stream=None):
+    """y = layer norm of the rows of x (over the last dimension) whose row_mask byte is not 0."""
+    call = _Call("tabx_layer_norm")
+    xr, rows, width = call.rows(x, "x")
+    yr, n, _ = call.rows(y, "y", width)
+    if n != rows:
+        call.refuse(f"y has {n} rows, x {rows}")
+    call.make(_lib.tabx_layer_norm, stream, rows, width, C.byref(xr),
+              call.array(row_mask, "row_mask", rows, torch.uint8),
+              call.array(weight, "weight", width, torch.float32),
+              call.array(bias, "bias", width, torch.float32), eps, C.byref(yr),
+              call.array(mean, "mean", rows, torch.float32),
+              call.array(rstd, "rstd", rows, torch.float32))
+
+
+def tabx_layer_norm_workspace(rows: int, width: int) -> int:
+    """Bytes of workspace that tabx_layer_norm_backward needs for the weight's and bias's gradients."""
+    n = _lib.tabx_layer_norm_workspace(rows, width)
+    if n < 0:
+        _check(n, "tabx_layer_norm_workspace")
+    return n
+
+
+def tabx_layer_norm_backward(x, weight, mean, rstd, grad_y, grad_x=None, grad_weight=None,
+                             grad_bias=None, workspace=None, row_mask=None, stream=None):
+    """The gradients of tabx_layer_norm; those that are None are not computed."""
+    call = _Call("tabx_layer_norm_backward")
+    xr, rows, width = call.rows(x, "x")
+    gr, n, _ = call.rows(grad_y, "grad_y", width)
+    if n != rows:
+        call.refuse(f"grad_y has {n} rows, x {rows}")
+    ir = None
+    if grad_x is not None:
+        ir, n, _ = call.rows(grad_x, "grad_x", width)
+        if n != rows:
+            call.refuse(f"grad_x has {n} rows, x {rows}")
+        ir = C.byref(ir)
+    size = 0 if workspace is None else workspace.numel()
+    call.make(_lib.tabx_layer_norm_backward, stream, rows, width, C.byref(xr),
+              call.array(row_mask, "row_mask", rows, torch.uint8),
+              call.array(weight, "weight", width, torch.float32),
+              call.needed(mean, "mean", rows, torch.float32),
+              call.needed(rstd, "rstd", rows, torch.float32), C.byref(gr), ir,
+              call.array(grad_weight, "grad_weight", width, torch.float32),
+              call.array(grad_bias, "grad_bias", width, torch.float32),
+              call.array(workspace, "workspace", size, torch.uint8), size)
+
+
+def tabx_sample_actions(logits, sampling, uniform, actions, log_prob=None, action_mask=None,
+                        controlled=None, stream=None):
+    """Draws an action from each unit's eight logits, into `actions` (uint8, in place)."""
+    call = _Call("tabx_sample_actions")
+    lr, rows, _ = call.rows(logits, "logits", 8)
+    call.make(_lib.tabx_sample_actions, stream, rows, C.byref(lr),
+              call.array(action_mask, "action_mask", rows, torch.uint8),
+              call.array(controlled, "controlled", rows, torch.uint8), C.byref(sampling),
+              call.needed(uniform, "uniform", rows, torch.float32),
+              call.needed(actions, "actions", rows, torch.uint8),
+              call.array(log_prob, "log_prob", rows, torch.float32))
+
+
+def tabx_sample_levels(scores, sampling, uniform, next_level, level_mask=None, env_mask=None,
+                       stream=None):
+    """Draws each env's next level from scores [levels] of all envs or [envs, levels] of each."""
+    call = _Call("tabx_sample_levels")
+    envs, shared = next_level.numel(), scores.dim() == 1
+    if scores.dim() == 2 and scores.stride(0) == 0:        # one row, expanded
+        scores, n, shared = scores[0], scores.shape[0], True
+        if n != envs:
+            call.refuse(f"scores has {n} rows, next_level {envs} elements")
+    sr, n, levels = call.rows(scores, "scores")
+    if shared:
+        sr.stride = 0
+    elif n != envs:
+        call.refuse(f"scores has {n} rows, next_level {envs} elements")
+    call.make(_lib.tabx_sample_levels, stream, envs, levels, C.byref(sr),
+              call.array(level_mask, "level_mask", levels, torch.uint8),
+              call.array(env_mask, "env_mask", envs, torch.uint8), C.byref(sampling),
+              call.needed(uniform, "uniform", envs, torch.float32),
+              call.needed(next_level, "next_level", envs, torch.int32))
+
+
+def tabx_action_log_prob(logits, actions, temperature, log_prob, entropy=None, action_mask=None,
+                         controlled=None, stream=None):
+    """log_prob (and entropy) of the actions under the distribution of their logits."""
+    call = _Call("tabx_action_log_prob")
+    lr, rows, _ = call.rows(logits, "logits", 8)
+    call.make(_lib.tabx_action_log_prob, stream, rows, C.byref(lr),
+              call.array(action_mask, "action_mask", rows, torch.uint8),
+              call.array(controlled, "controlled", rows, torch.uint8),
+              call.needed(actions, "actions", rows, torch.uint8), temperature,
+              call.needed(log_prob, "log_prob", rows, torch.float32),
+              call.array(entropy, "entropy", rows, torch.float32))
+
+
+def tabx_action_log_prob_backward(logits, actions, temperature, grad_log_prob, grad_entropy,
+                                  grad_logits, action_mask=None, controlled=None, stream=None):
+    """The logits' gradient, from those of log_prob and entropy (either may be None: zero)."""
+    call = _Call("tabx_action_log_prob_backward")
+    lr, rows, _ = call.rows(logits, "logits", 8)
+    gr, n, _ = call.rows(grad_logits, "grad_logits", 8)
+    if n != rows:
+        call.refuse(f"grad_logits has {n} rows, logits {rows}")
+    call.make(_lib.tabx_action_log_prob_backward, stream, rows, C.byref(lr),
+              call.array(action_mask, "action_mask", rows, torch.uint8),
+              call.array(controlled, "controlled", rows, torch.uint8),
+              call.needed(actions, "actions", rows, torch.uint8), temperature,
+              call.array(grad_log_prob, "grad_log_prob", rows, torch.float32),
+              call.array(grad_entropy, "grad_entropy", rows, torch.float32), C.byref(gr))
 
 
 class TabxEnv:
@@ -414,6 +636,23 @@ class TabxEnv:
     def step_observe(self, actions, stream=None):
         tabx_step_observe(self.params, self.scenario, self.state, actions, self.rewards,
                           self.dones, self.obs, self.vis, self.amask, stream)
+
+    def norm_obs(self, weight, bias, eps, y, mean=None, rstd=None, controlled=None, stream=None):
+        """y [E, N, D] = layer norm of the observation rows, of the controlled units (None: all)."""
+        tabx_layer_norm(self.obs, weight, bias, eps, y, mean, rstd, controlled, stream)
+
+    def sample_actions(self, logits, sampling, uniform, actions, log_prob=None, controlled=None,
+                       stream=None):
+        """Fills `actions` (uint8 [E, N], in place) for the controlled units (None: all) from their
+        logits [E, N, 8], where the last observation lets them strike."""
+        tabx_sample_actions(logits, sampling, uniform, actions, log_prob, self.amask, controlled,
+                            stream)
+        return actions
+
+    def sample_levels(self, scores, sampling, uniform, level_mask=None, env_mask=None, stream=None):
+        """Draws the levels that the envs' next episodes take (instead of the uniform draw)."""
+        tabx_sample_levels(scores, sampling, uniform, self.st["next_level"], level_mask, env_mask,
+                           stream)
 
     def snapshot(self) -> dict:
         return {k: v.clone() for k, v in self.st.items()}

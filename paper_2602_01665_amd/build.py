@@ -7,11 +7,13 @@ import sys
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
-SOURCES = [os.path.join(_PKG, "csrc", "tabx_kernels.hip")]
+SOURCES = [os.path.join(_PKG, "csrc", "tabx_kernels.hip")]              # the tick
+LEARNER_SOURCES = [os.path.join(_PKG, "csrc", "tabx_learner.hip")]      # the learner's side of it
 HEADERS = [os.path.join(_ROOT, "include", "tabx.h")] + [
     os.path.join(_PKG, "csrc", h)
     for h in ("tabx_device.h", "tabx_policy.h", "tabx_step.h", "tabx_observe.h",
-              "tabx_observe_packed.h")]
+              "tabx_observe_packed.h", "tabx_rows.h", "tabx_norm.h", "tabx_sample.h",
+              "tabx_levels.h")]
 LIB_PATH = os.path.join(_PKG, "libtabx.so")
 
 HIPCC_FLAGS = [
@@ -25,7 +27,7 @@ HIPCC_FLAGS = [
 
 def build(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc] + HIPCC_FLAGS + SOURCES + ["-o", LIB_PATH]
+    cmd = [hipcc] + HIPCC_FLAGS + SOURCES + LEARNER_SOURCES + ["-o", LIB_PATH]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
@@ -36,7 +38,7 @@ def is_stale() -> bool:
     if not os.path.exists(LIB_PATH):
         return True
     t = os.path.getmtime(LIB_PATH)
-    return any(os.path.getmtime(f) > t for f in SOURCES + HEADERS)
+    return any(os.path.getmtime(f) > t for f in SOURCES + LEARNER_SOURCES + HEADERS)
 
 
 if __name__ == "__main__":

@@ -1179,10 +1179,10 @@ const char *tabx_strerror(int code)
     switch (code) {
     case TABX_OK: return "ok";
     case TABX_ERR_NULL: return "a required pointer is NULL (or an optional one does not match the shape)";
-    case TABX_ERR_SHAPE: return "unsupported shape (num_units, max_zones, grid, max_steps or num_envs)";
+    case TABX_ERR_SHAPE: return "unsupported shape (num_units, max_zones, grid, max_steps or num_envs; rows, width, stride or type)";
     case TABX_ERR_ALIGN: return "a pointer is not aligned as required";
     case TABX_ERR_LAUNCH: return "the HIP runtime refused the kernel launch";
-    case TABX_ERR_PARAM: return "a physics constant is not finite or not positive";
+    case TABX_ERR_PARAM: return "a physics constant or a setting is out of its range";
     default: return "unknown error code";
     }
 }
