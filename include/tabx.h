@@ -402,7 +402,7 @@ typedef struct TabxRows {
     int32_t  type;             /* TabxType                                                 */
 } TabxRows;
 
-#define TABX_NORM_MAX_WIDTH 16384     /* widest row of the layer norm                      */
+#define TABX_NORM_MAX_WIDTH 8192      /* widest row of the layer norm                      */
 #define TABX_SAMPLE_MAX_LEVELS 16384  /* most levels tabx_sample_levels chooses between    */
 
 /* Layer norm of every row with row_mask[r] != 0 (NULL: all; pass `controlled` to leave out the

@@ -267,100 +267,111 @@ def tabx_scripted_step_observe(params, scenario, state, policy, memory, controll
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
-class _Call:
-    """The arguments of one call as the library takes them.  Every tensor has to be on one GPU."""
+# What a call on a few thousand rows costs is the time until it is enqueued: the checks are plain
+# functions of few steps (a small tabx_sample_actions takes the host 6.0 us, 10.0 as methods of an
+# object with torch.cuda.current_stream()).  `device` is that of a call's first tensor, -1 the host.
 
-    def __init__(self, what: str):
-        self.what, self.device, self.host = what, None, None
 
-    def refuse(self, why: str):
-        raise TabxError(f"{self.what}: {why}")
+def _refuse(what, why):
+    raise TabxError(f"{what}: {why}")
 
-    def _place(self, t, name):
-        d = t.device
-        if self.device is None:
-            self.device = d
-        elif d != self.device:
-            self.refuse(f"{name} is on {d}, not on {self.device}")
-        if d.type != "cuda":
-            self.host = name               # (refused last, after what is wrong with its shape)
 
-    def rows(self, t, name, width=0):
-        """(TabxRows, rows, width) of a tensor [..., width] whose rows lie at equal distances."""
-        code = TYPES.get(t.dtype)
-        if code is None:
-            self.refuse(f"{name} is {t.dtype}, not one of float32, bfloat16, float16")
-        n = t.dim()
-        if n < 1:
-            self.refuse(f"{name} has no dimensions")
-        shape, stride = t.shape, t.stride()
-        wide = shape[-1]
-        if width and wide != width:
-            self.refuse(f"{name} has rows of {wide} elements, not {width}")
-        if wide > 1 and stride[-1] != 1:
-            self.refuse(f"the elements of a row of {name} are not next to each other")
-        count, apart = 1, 0
-        for k in range(n - 2, -1, -1):     # the leading dimensions have to be one run of rows
-            if shape[k] == 1:
-                continue
-            if apart == 0:
-                apart = stride[k]
-            elif stride[k] != apart * count:
-                self.refuse(f"the rows of {name} do not lie at equal distances")
-            count *= shape[k]
-        if count > 1 and apart < wide:
-            self.refuse(f"the rows of {name} overlap")
-        self._place(t, name)
-        return TabxRows(t.data_ptr(), max(apart, wide), code), count, wide
+def _elsewhere(what, t, name, device):
+    place = "cpu" if device < 0 else f"cuda:{device}"
+    _refuse(what, f"{name} is on {t.device}, not on {place}")
 
-    def array(self, t, name, count, dtype):
-        """Address of a contiguous tensor of `count` elements, None for None."""
-        if t is None:
-            return None
-        if t.dtype is not dtype:
-            self.refuse(f"{name} is {t.dtype}, not {dtype}")
-        if t.numel() != count:
-            self.refuse(f"{name} has {t.numel()} elements, not {count}")
-        if not t.is_contiguous():
-            self.refuse(f"{name} is not contiguous")
-        self._place(t, name)
-        return t.data_ptr()
 
-    def needed(self, t, name, count, dtype):
-        if t is None:
-            self.refuse(f"{name} is needed")
-        return self.array(t, name, count, dtype)
+def _rows(what, t, name, width, device=None):
+    """(TabxRows, rows) of a tensor [..., width] whose rows lie at equal distances."""
+    code = TYPES.get(t.dtype)
+    if code is None:
+        _refuse(what, f"{name} is {t.dtype}, not one of float32, bfloat16, float16")
+    shape = t.shape
+    if not shape:
+        _refuse(what, f"{name} has no dimensions")
+    wide = shape[-1]
+    if wide != width and width:
+        _refuse(what, f"{name} has rows of {wide} elements, not {width}")
+    if device is not None and t.get_device() != device:
+        _elsewhere(what, t, name, device)
+    if t.is_contiguous():
+        return TabxRows(t.data_ptr(), wide, code), t.numel() // wide if wide else 0
+    stride = t.stride()
+    if wide > 1 and stride[-1] != 1:
+        _refuse(what, f"the elements of a row of {name} are not next to each other")
+    count, apart = 1, 0
+    for k in range(len(shape) - 2, -1, -1):    # the leading dimensions have to be one run of rows
+        if shape[k] == 1:
+            continue
+        if count == 1:
+            apart = stride[k]
+        elif stride[k] != apart * count:
+            _refuse(what, f"the rows of {name} do not lie at equal distances")
+        count *= shape[k]
+    if count > 1 and apart < wide:
+        _refuse(what, f"the rows of {name} overlap")
+    return TabxRows(t.data_ptr(), max(apart, wide), code), count
 
-    def make(self, function, stream, *args):
-        if self.host is not None:
-            self.refuse(f"{self.host} is not on a GPU")
-        here = torch.cuda.current_device()
-        if stream is None:
-            stream = torch.cuda.current_stream(self.device)
-        elif stream.device != self.device:
-            self.refuse(f"the stream is on {stream.device}, the tensors on {self.device}")
-        if self.device.index == here:
-            rc = function(*args, stream.cuda_stream)
-        else:
-            with torch.cuda.device(self.device):
-                rc = function(*args, stream.cuda_stream)
-        if rc != 0:
-            _check(rc, self.what)
+
+def _same_rows(what, t, name, width, device, rows):
+    """The same for a tensor that has to have as many rows."""
+    r, n = _rows(what, t, name, width, device)
+    if n != rows:
+        _refuse(what, f"{name} has {n} rows, not {rows}")
+    return r
+
+
+def _array(what, t, name, count, dtype, device):
+    """Address of a contiguous tensor of `count` elements, None for None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype:
+        _refuse(what, f"{name} is {t.dtype}, not {dtype}")
+    if t.numel() != count:
+        _refuse(what, f"{name} has {t.numel()} elements, not {count}")
+    if not t.is_contiguous():
+        _refuse(what, f"{name} is not contiguous")
+    if t.get_device() != device:
+        _elsewhere(what, t, name, device)
+    return t.data_ptr()
+
+
+def _needed(what, t, name, count, dtype, device):
+    if t is None:
+        _refuse(what, f"{name} is needed")
+    return _array(what, t, name, count, dtype, device)
+
+
+def _enqueue(what, function, device, stream, *args):
+    if device < 0:
+        _refuse(what, "the tensors are not on a GPU")
+    if stream is None:
+        raw = torch._C._cuda_getCurrentRawStream(device)
+    elif stream.device_index == device:
+        raw = stream.cuda_stream
+    else:
+        _refuse(what, f"the stream is on {stream.device}, the tensors are on cuda:{device}")
+    if torch.cuda.current_device() == device:
+        rc = function(*args, raw)
+    else:
+        with torch.cuda.device(device):
+            rc = function(*args, raw)
+    if rc != 0:
+        _check(rc, what)
 
 
 def tabx_layer_norm(x, weight, bias, eps, y, mean=None, rstd=None, row_mask=None, stream=None):
     """y = layer norm of the rows of x (over the last dimension) whose row_mask byte is not 0."""
-    call = _Call("tabx_layer_norm")
-    xr, rows, width = call.rows(x, "x")
-    yr, n, _ = call.rows(y, "y", width)
-    if n != rows:
-        call.refuse(f"y has {n} rows, x {rows}")
-    call.make(_lib.tabx_layer_norm, stream, rows, width, C.byref(xr),
-              call.array(row_mask, "row_mask", rows, torch.uint8),
-              call.array(weight, "weight", width, torch.float32),
-              call.array(bias, "bias", width, torch.float32), eps, C.byref(yr),
-              call.array(mean, "mean", rows, torch.float32),
-              call.array(rstd, "rstd", rows, torch.float32))
+    what, f32, dev = "tabx_layer_norm", torch.float32, x.get_device()
+    xr, rows = _rows(what, x, "x", 0)
+    width = x.shape[-1]
+    yr = _same_rows(what, y, "y", width, dev, rows)
+    _enqueue(what, _lib.tabx_layer_norm, dev, stream, rows, width, C.byref(xr),
+             _array(what, row_mask, "row_mask", rows, torch.uint8, dev),
+             _array(what, weight, "weight", width, f32, dev),
+             _array(what, bias, "bias", width, f32, dev), eps, C.byref(yr),
+             _array(what, mean, "mean", rows, f32, dev),
+             _array(what, rstd, "rstd", rows, f32, dev))
 
 
 def tabx_layer_norm_workspace(rows: int, width: int) -> int:
@@ -374,89 +385,86 @@ def tabx_layer_norm_workspace(rows: int, width: int) -> int:
 def tabx_layer_norm_backward(x, weight, mean, rstd, grad_y, grad_x=None, grad_weight=None,
                              grad_bias=None, workspace=None, row_mask=None, stream=None):
     """The gradients of tabx_layer_norm; those that are None are not computed."""
-    call = _Call("tabx_layer_norm_backward")
-    xr, rows, width = call.rows(x, "x")
-    gr, n, _ = call.rows(grad_y, "grad_y", width)
-    if n != rows:
-        call.refuse(f"grad_y has {n} rows, x {rows}")
+    what, f32, dev = "tabx_layer_norm_backward", torch.float32, x.get_device()
+    xr, rows = _rows(what, x, "x", 0)
+    width = x.shape[-1]
+    gr = _same_rows(what, grad_y, "grad_y", width, dev, rows)
     ir = None
     if grad_x is not None:
-        ir, n, _ = call.rows(grad_x, "grad_x", width)
-        if n != rows:
-            call.refuse(f"grad_x has {n} rows, x {rows}")
-        ir = C.byref(ir)
+        ir = C.byref(_same_rows(what, grad_x, "grad_x", width, dev, rows))
     size = 0 if workspace is None else workspace.numel()
-    call.make(_lib.tabx_layer_norm_backward, stream, rows, width, C.byref(xr),
-              call.array(row_mask, "row_mask", rows, torch.uint8),
-              call.array(weight, "weight", width, torch.float32),
-              call.needed(mean, "mean", rows, torch.float32),
-              call.needed(rstd, "rstd", rows, torch.float32), C.byref(gr), ir,
-              call.array(grad_weight, "grad_weight", width, torch.float32),
-              call.array(grad_bias, "grad_bias", width, torch.float32),
-              call.array(workspace, "workspace", size, torch.uint8), size)
+    _enqueue(what, _lib.tabx_layer_norm_backward, dev, stream, rows, width, C.byref(xr),
+             _array(what, row_mask, "row_mask", rows, torch.uint8, dev),
+             _array(what, weight, "weight", width, f32, dev),
+             _needed(what, mean, "mean", rows, f32, dev),
+             _needed(what, rstd, "rstd", rows, f32, dev), C.byref(gr), ir,
+             _array(what, grad_weight, "grad_weight", width, f32, dev),
+             _array(what, grad_bias, "grad_bias", width, f32, dev),
+             _array(what, workspace, "workspace", size, torch.uint8, dev), size)
 
 
 def tabx_sample_actions(logits, sampling, uniform, actions, log_prob=None, action_mask=None,
                         controlled=None, stream=None):
     """Draws an action from each unit's eight logits, into `actions` (uint8, in place)."""
-    call = _Call("tabx_sample_actions")
-    lr, rows, _ = call.rows(logits, "logits", 8)
-    call.make(_lib.tabx_sample_actions, stream, rows, C.byref(lr),
-              call.array(action_mask, "action_mask", rows, torch.uint8),
-              call.array(controlled, "controlled", rows, torch.uint8), C.byref(sampling),
-              call.needed(uniform, "uniform", rows, torch.float32),
-              call.needed(actions, "actions", rows, torch.uint8),
-              call.array(log_prob, "log_prob", rows, torch.float32))
+    what, f32, u8, dev = "tabx_sample_actions", torch.float32, torch.uint8, logits.get_device()
+    lr, rows = _rows(what, logits, "logits", 8)
+    _enqueue(what, _lib.tabx_sample_actions, dev, stream, rows, C.byref(lr),
+             _array(what, action_mask, "action_mask", rows, u8, dev),
+             _array(what, controlled, "controlled", rows, u8, dev), C.byref(sampling),
+             _needed(what, uniform, "uniform", rows, f32, dev),
+             _needed(what, actions, "actions", rows, u8, dev),
+             _array(what, log_prob, "log_prob", rows, f32, dev))
 
 
 def tabx_sample_levels(scores, sampling, uniform, next_level, level_mask=None, env_mask=None,
                        stream=None):
     """Draws each env's next level from scores [levels] of all envs or [envs, levels] of each."""
-    call = _Call("tabx_sample_levels")
-    envs, shared = next_level.numel(), scores.dim() == 1
-    if scores.dim() == 2 and scores.stride(0) == 0:        # one row, expanded
-        scores, n, shared = scores[0], scores.shape[0], True
-        if n != envs:
-            call.refuse(f"scores has {n} rows, next_level {envs} elements")
-    sr, n, levels = call.rows(scores, "scores")
-    if shared:
+    what, u8, dev = "tabx_sample_levels", torch.uint8, scores.get_device()
+    envs, n = next_level.numel(), scores.dim()
+    if n > 2:
+        _refuse(what, f"scores has {n} dimensions")
+    if n == 2:
+        if scores.shape[0] != envs:
+            _refuse(what, f"scores has {scores.shape[0]} rows, next_level {envs} elements")
+        if envs and scores.stride(0) == 0:     # one row, expanded
+            scores, n = scores[0], 1
+    sr, _ = _rows(what, scores, "scores", 0)
+    levels = scores.shape[-1]
+    if n == 1:
         sr.stride = 0
-    elif n != envs:
-        call.refuse(f"scores has {n} rows, next_level {envs} elements")
-    call.make(_lib.tabx_sample_levels, stream, envs, levels, C.byref(sr),
-              call.array(level_mask, "level_mask", levels, torch.uint8),
-              call.array(env_mask, "env_mask", envs, torch.uint8), C.byref(sampling),
-              call.needed(uniform, "uniform", envs, torch.float32),
-              call.needed(next_level, "next_level", envs, torch.int32))
+    _enqueue(what, _lib.tabx_sample_levels, dev, stream, envs, levels, C.byref(sr),
+             _array(what, level_mask, "level_mask", levels, u8, dev),
+             _array(what, env_mask, "env_mask", envs, u8, dev), C.byref(sampling),
+             _needed(what, uniform, "uniform", envs, torch.float32, dev),
+             _needed(what, next_level, "next_level", envs, torch.int32, dev))
 
 
 def tabx_action_log_prob(logits, actions, temperature, log_prob, entropy=None, action_mask=None,
                          controlled=None, stream=None):
     """log_prob (and entropy) of the actions under the distribution of their logits."""
-    call = _Call("tabx_action_log_prob")
-    lr, rows, _ = call.rows(logits, "logits", 8)
-    call.make(_lib.tabx_action_log_prob, stream, rows, C.byref(lr),
-              call.array(action_mask, "action_mask", rows, torch.uint8),
-              call.array(controlled, "controlled", rows, torch.uint8),
-              call.needed(actions, "actions", rows, torch.uint8), temperature,
-              call.needed(log_prob, "log_prob", rows, torch.float32),
-              call.array(entropy, "entropy", rows, torch.float32))
+    what, f32, u8, dev = "tabx_action_log_prob", torch.float32, torch.uint8, logits.get_device()
+    lr, rows = _rows(what, logits, "logits", 8)
+    _enqueue(what, _lib.tabx_action_log_prob, dev, stream, rows, C.byref(lr),
+             _array(what, action_mask, "action_mask", rows, u8, dev),
+             _array(what, controlled, "controlled", rows, u8, dev),
+             _needed(what, actions, "actions", rows, u8, dev), temperature,
+             _needed(what, log_prob, "log_prob", rows, f32, dev),
+             _array(what, entropy, "entropy", rows, f32, dev))
 
 
 def tabx_action_log_prob_backward(logits, actions, temperature, grad_log_prob, grad_entropy,
                                   grad_logits, action_mask=None, controlled=None, stream=None):
     """The logits' gradient, from those of log_prob and entropy (either may be None: zero)."""
-    call = _Call("tabx_action_log_prob_backward")
-    lr, rows, _ = call.rows(logits, "logits", 8)
-    gr, n, _ = call.rows(grad_logits, "grad_logits", 8)
-    if n != rows:
-        call.refuse(f"grad_logits has {n} rows, logits {rows}")
-    call.make(_lib.tabx_action_log_prob_backward, stream, rows, C.byref(lr),
-              call.array(action_mask, "action_mask", rows, torch.uint8),
-              call.array(controlled, "controlled", rows, torch.uint8),
-              call.needed(actions, "actions", rows, torch.uint8), temperature,
-              call.array(grad_log_prob, "grad_log_prob", rows, torch.float32),
-              call.array(grad_entropy, "grad_entropy", rows, torch.float32), C.byref(gr))
+    what, f32, u8 = "tabx_action_log_prob_backward", torch.float32, torch.uint8
+    dev = logits.get_device()
+    lr, rows = _rows(what, logits, "logits", 8)
+    gr = _same_rows(what, grad_logits, "grad_logits", 8, dev, rows)
+    _enqueue(what, _lib.tabx_action_log_prob_backward, dev, stream, rows, C.byref(lr),
+             _array(what, action_mask, "action_mask", rows, u8, dev),
+             _array(what, controlled, "controlled", rows, u8, dev),
+             _needed(what, actions, "actions", rows, u8, dev), temperature,
+             _array(what, grad_log_prob, "grad_log_prob", rows, f32, dev),
+             _array(what, grad_entropy, "grad_entropy", rows, f32, dev), C.byref(gr))
 
 
 class TabxEnv:

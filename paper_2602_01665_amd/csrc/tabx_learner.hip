@@ -59,58 +59,109 @@ static int launched(hipError_t err)
 }
 
 template <typename Args>
-static int launch(void (*kernel)(Args), int64_t groups, int64_t most, int threads, size_t lds, const Args &a, void *stream)
+static int launch(void (*kernel)(Args), int64_t groups, int threads, const Args &a, void *stream)
 {
     void *args[] = {(void *)&a};
-    return launched(hipLaunchKernel((const void *)kernel, dim3((unsigned)(groups < most ? groups : most)), dim3((unsigned)threads),
-                                    args, lds, (hipStream_t)stream));
+    return launched(hipLaunchKernel((const void *)kernel, dim3((unsigned)groups), dim3((unsigned)threads), args, 0,
+                                    (hipStream_t)stream));
 }
 
 // --- layer norm ---------------------------------------------------------------------------------
 
-constexpr int64_t kMostGroups = (int64_t)1 << 20;   // beyond them a workgroup takes several turns
+constexpr int64_t kComputeUnits = 256;
+constexpr int64_t kL2Bytes = 32 << 20;             // eight L2s of 4 MB
+constexpr int64_t kSideCacheBytes = 256 << 20;     // the cache on the memory's side
+constexpr int64_t kMostGroups = (int64_t)1 << 20;  // of a launch; beyond them its teams or lanes take several turns
+constexpr int64_t kNormTeams = 81920;              // teams that share the rows of a forward call, if they are many
+constexpr int64_t kGradTurns = 4;                  // turns of a team's run of rows in a backward call
 
-static int norm_forward(const NormArgs &a, void *stream)
+static int64_t quotient_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+static int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
+static int64_t size_of(int type) { return type == TABX_F32 ? 4 : 2; }
+
+// Teams of a workgroup, and rows that a team works on at a time.
+constexpr int teams_of(int lanes) { return lanes <= 64 ? threads_of(lanes) / 64 : 1; }
+constexpr int at_once(int lanes) { return lanes < 64 ? 64 / lanes : 1; }
+
+// Calls F<LANES, PIECES>::go for the first form that holds rows of that many pieces; the rows fill all of its pieces
+// but the last in all lanes, as the kernels take for granted.
+template <template <int, int> class F, typename... Args>
+static int for_width(int pieces, const Args &...args)
 {
-    const int pieces = (a.width + 3) / 4;
-#define TABX_NORM(LANES, PIECES)                                                                          \
-    if (pieces <= LANES * PIECES) {                                                                       \
-        constexpr int threads = LANES > 256 ? LANES : 256, rows = threads / LANES;                        \
-        return launch(tabx_norm_kernel<LANES, PIECES>, (a.rows + rows - 1) / rows, kMostGroups, threads, 0, a, stream); \
-    }
-    TABX_NORM(8, 1) TABX_NORM(8, 2) TABX_NORM(8, 3) TABX_NORM(8, 4)
-    TABX_NORM(16, 3) TABX_NORM(16, 4)
-    TABX_NORM(32, 3) TABX_NORM(32, 4)
-    TABX_NORM(64, 3) TABX_NORM(64, 4)
-    TABX_NORM(256, 2) TABX_NORM(256, 3) TABX_NORM(256, 4)
-    TABX_NORM(1024, 2) TABX_NORM(1024, 3) TABX_NORM(1024, 4)
-#undef TABX_NORM
+#define TABX_FORM(LANES, PIECES)                                                        \
+    if constexpr (F<LANES, PIECES>::kUsed)                                              \
+        if (pieces <= LANES * PIECES) {                                                 \
+            if (pieces <= LANES * (PIECES - 1)) return TABX_ERR_SHAPE;                  \
+            return F<LANES, PIECES>::go(args...);                                       \
+        }
+    TABX_FORM(1, 1)
+    TABX_FORM(16, 1) TABX_FORM(16, 2) TABX_FORM(16, 3) TABX_FORM(32, 2) TABX_FORM(32, 3)
+    TABX_FORM(64, 2) TABX_FORM(64, 3) TABX_FORM(64, 4) TABX_FORM(128, 3)
+    TABX_FORM(256, 2) TABX_FORM(256, 3) TABX_FORM(256, 4) TABX_FORM(1024, 2)
+#undef TABX_FORM
+    static_assert(TABX_NORM_MAX_WIDTH == 4 * 1024 * 2, "the widest form");
     return TABX_ERR_SHAPE;
 }
 
-// Rows a workgroup of the backward pass works on at a time.
-static int grad_rows(int32_t width)
-{
-    const int pieces = (width + 3) / 4;
-    return pieces <= 32 ? 32 : pieces <= 64 ? 16 : pieces <= 128 ? 8 : pieces <= 256 ? 4 : 1;
-}
+// A team takes its rows in one turn or two and is done, but for the widest rows: there every workgroup would load as much
+// of weight and bias as it has rows, so the machine's lanes stay (rows of 4096: 74 us, 63; of 6000: 139, 102; rows of 2144
+// are faster without, 250 and 261).
+// What is written and is more than the L2s hold goes past them (22 MB on from where they are full: 28.6 us, 23.1; 10v10 x
+// 16384: 76 us, 71), but in pieces of a third of a line it does not (rows of 184 elements: 85 us, 87; of 186: 87.6, 91.5).
+template <int LANES, int PIECES>
+struct NormForward {
+    static constexpr bool kUsed = true;
+    static int go(NormArgs a, void *stream)
+    {
+        constexpr int teams = teams_of(LANES);
+        constexpr bool stays = LANES * PIECES > 768;
+        a.team_rows = LANES <= 64 ? least(quotient_up(quotient_up(a.rows, kNormTeams), at_once(LANES)) * at_once(LANES), 64) : 1;
+        const int64_t groups = least(quotient_up(a.rows, a.team_rows * teams), stays ? kComputeUnits * 2048 / LANES : kMostGroups);
+        a.lap = groups * teams * a.team_rows;
+        a.stream = !(LANES == 16 && PIECES == 3) && a.rows * a.width * size_of(a.y_type) > kL2Bytes;
+        return a.x_type == TABX_F32 ? launch(tabx_norm_kernel<LANES, PIECES, 4>, groups, threads_of(LANES), a, stream)
+                                    : launch(tabx_norm_kernel<LANES, PIECES, 2>, groups, threads_of(LANES), a, stream);
+    }
+};
 
-// Workgroups that add up rows side by side: a workgroup has at least four turns, and the parts stay few.
-static int64_t grad_groups(int64_t rows, int32_t width)
-{
-    const int64_t turns = (rows + grad_rows(width) - 1) / grad_rows(width);
-    const int64_t groups = (turns + 3) / 4;
-    return groups < 1024 ? (groups < 1 ? 1 : groups) : 1024;
-}
+// Workgroups of the backward pass, which add up rows side by side: as many as the machine holds at a time, so that all
+// take as long (a third more of them than it holds: 206 us, 197, 200000 rows of 700), and few enough that each team has a
+// whole run of rows to add up.  The forms of three pieces for fewer lanes gain nothing here.
+template <int LANES, int PIECES>
+struct GradGroups {
+    static constexpr bool kUsed = LANES > 32 || PIECES < 3;
+    static int go(int64_t rows)
+    {
+        constexpr int64_t most = kComputeUnits * 4 * grad_wavefronts(PIECES) * 64 / threads_of(LANES);
+        const int64_t groups = quotient_up(rows, kGradTurns * at_once(LANES) * teams_of(LANES));
+        return (int)(groups < 1 ? 1 : least(groups, most));
+    }
+};
+
+static int grad_groups(int64_t rows, int32_t width) { return for_width<GradGroups>((width + 3) / 4, rows); }
 
 template <int LANES, int PIECES>
-static int launch_grad(const NormArgs &a, int64_t groups, void *stream)
-{
-    constexpr int threads = LANES > 256 ? LANES : 256;
-    if (a.y && a.partial) return launch(tabx_norm_grad_kernel<LANES, PIECES, true, true>, groups, groups, threads, 0, a, stream);
-    if (a.y) return launch(tabx_norm_grad_kernel<LANES, PIECES, true, false>, groups, groups, threads, 0, a, stream);
-    return launch(tabx_norm_grad_kernel<LANES, PIECES, false, true>, groups, groups, threads, 0, a, stream);
-}
+struct NormBackward {
+    static constexpr bool kUsed = GradGroups<LANES, PIECES>::kUsed;
+    template <int X_BYTES, int G_BYTES>
+    static int with_types(const NormArgs &a, int64_t groups, void *stream)
+    {
+        const bool once = a.rows * a.width * (X_BYTES + G_BYTES) > kSideCacheBytes;
+        return launch(a.y    ? tabx_norm_grad_kernel<LANES, PIECES, X_BYTES, G_BYTES, true, false>
+                      : once ? tabx_norm_grad_kernel<LANES, PIECES, X_BYTES, G_BYTES, false, true>
+                             : tabx_norm_grad_kernel<LANES, PIECES, X_BYTES, G_BYTES, false, false>,
+                      groups, threads_of(LANES), a, stream);
+    }
+    static int go(NormArgs a, int64_t groups, void *stream)
+    {
+        constexpr int turns_at_once = at_once(LANES);
+        a.team_rows = least(quotient_up(quotient_up(a.rows, groups * teams_of(LANES)), turns_at_once), kGradTurns) * turns_at_once;
+        a.team_rows = least(a.team_rows, 64);
+        a.lap = groups * teams_of(LANES) * a.team_rows;
+        if (a.x_type == TABX_F32) return a.g_type == TABX_F32 ? with_types<4, 4>(a, groups, stream) : with_types<4, 2>(a, groups, stream);
+        return a.g_type == TABX_F32 ? with_types<2, 4>(a, groups, stream) : with_types<2, 2>(a, groups, stream);
+    }
+};
 
 static int norm_join(const float *partial, int parts, int width, float *grad_weight, float *grad_bias, void *stream)
 {
@@ -121,26 +172,13 @@ static int norm_join(const float *partial, int parts, int width, float *grad_wei
 
 static int norm_backward(const NormArgs &a, float *grad_weight, float *grad_bias, void *stream)
 {
-    const int pieces = (a.width + 3) / 4;
     const int64_t groups = grad_groups(a.rows, a.width);
-    int rc = TABX_ERR_SHAPE;
-    if (pieces <= 8) rc = launch_grad<8, 1>(a, groups, stream);
-    else if (pieces <= 16) rc = launch_grad<8, 2>(a, groups, stream);
-    else if (pieces <= 24) rc = launch_grad<8, 3>(a, groups, stream);
-    else if (pieces <= 32) rc = launch_grad<8, 4>(a, groups, stream);
-    else if (pieces <= 48) rc = launch_grad<16, 3>(a, groups, stream);
-    else if (pieces <= 64) rc = launch_grad<16, 4>(a, groups, stream);
-    else if (pieces <= 96) rc = launch_grad<32, 3>(a, groups, stream);
-    else if (pieces <= 128) rc = launch_grad<32, 4>(a, groups, stream);
-    else if (pieces <= 192) rc = launch_grad<64, 3>(a, groups, stream);
-    else if (pieces <= 256) rc = launch_grad<64, 4>(a, groups, stream);
-    else if (pieces <= 512) rc = launch_grad<256, 2>(a, groups, stream);
-    else if (pieces <= 768) rc = launch_grad<256, 3>(a, groups, stream);
-    else if (pieces <= 1024) rc = launch_grad<256, 4>(a, groups, stream);
-    else if (pieces <= 2048) rc = launch_grad<1024, 2>(a, groups, stream);
-    else if (pieces <= 4096) rc = launch_grad<1024, 4>(a, groups, stream);
+    const int rc = for_width<NormBackward>((a.width + 3) / 4, a, groups, stream);
     return rc != TABX_OK || !a.partial ? rc : norm_join(a.partial, (int)groups, a.width, grad_weight, grad_bias, stream);
 }
+
+// Workgroups of a launch of one lane per row.
+static int64_t lane_groups(int64_t rows) { return least(quotient_up(rows, 256), kMostGroups); }
 
 // --- draws --------------------------------------------------------------------------------------
 
@@ -202,14 +240,14 @@ int tabx_layer_norm(int64_t rows, int32_t width, const TabxRows *x, const uint8_
     a.row_mask = row_mask;
     a.weight = weight, a.bias = bias, a.mean = mean, a.rstd = rstd;
     a.rows = rows, a.width = width, a.eps = eps, a.inv_width = 1.0f / (float)width;
-    return norm_forward(a, stream);
+    return for_width<NormForward>((width + 3) / 4, a, stream);
 }
 
 int64_t tabx_layer_norm_workspace(int64_t rows, int32_t width)
 {
     const int rc = tabx::check_rows(rows, width);
     if (rc || width > TABX_NORM_MAX_WIDTH) return TABX_ERR_SHAPE;
-    return tabx::grad_groups(rows, width) * 2 * width * (int64_t)sizeof(float);
+    return (int64_t)tabx::grad_groups(rows, width) * 2 * width * (int64_t)sizeof(float);
 }
 
 int tabx_layer_norm_backward(int64_t rows, int32_t width, const TabxRows *x, const uint8_t *row_mask, const float *weight,
@@ -260,7 +298,7 @@ int tabx_sample_actions(int64_t rows, const TabxRows *logits, const uint8_t *act
     a.uniform = uniform;
     a.actions_out = actions;
     a.log_prob = log_prob;
-    return launch(tabx_sample_actions_kernel, (rows + 255) / 256, kMostGroups, 256, 0, a, stream);
+    return launch(tabx_sample_actions_kernel, lane_groups(rows), 256, a, stream);
 }
 
 int tabx_sample_levels(int64_t envs, int32_t num_levels, const TabxRows *scores, const uint8_t *level_mask,
@@ -306,7 +344,7 @@ int tabx_action_log_prob(int64_t rows, const TabxRows *logits, const uint8_t *ac
     a.actions = actions;
     a.log_prob = log_prob;
     a.entropy = entropy;
-    return launch(tabx_log_prob_kernel, (rows + 255) / 256, kMostGroups, 256, 0, a, stream);
+    return launch(tabx_log_prob_kernel, lane_groups(rows), 256, a, stream);
 }
 
 int tabx_action_log_prob_backward(int64_t rows, const TabxRows *logits, const uint8_t *action_mask, const uint8_t *controlled,
@@ -327,7 +365,7 @@ int tabx_action_log_prob_backward(int64_t rows, const TabxRows *logits, const ui
     a.grad_logits = grad_logits->data;
     a.grad_stride = grad_logits->stride;
     a.grad_type = grad_logits->type;
-    return launch(tabx_log_prob_grad_kernel, (rows + 255) / 256, kMostGroups, 256, 0, a, stream);
+    return launch(tabx_log_prob_grad_kernel, lane_groups(rows), 256, a, stream);
 }
 
 } // extern "C"

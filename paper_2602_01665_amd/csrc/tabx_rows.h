@@ -9,6 +9,7 @@
 namespace tabx {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
@@ -27,12 +28,15 @@ __device__ __forceinline__ f32x4 load_four(const typename Element<TYPE>::one *at
     return __builtin_convertvector(v, f32x4);
 }
 
-// To the element's type: one rounding, to nearest even.
-template <int TYPE>
+// To the element's type: one rounding, to nearest even.  STREAM: past the caches.
+template <int TYPE, bool STREAM = false>
 __device__ __forceinline__ void store_four(typename Element<TYPE>::one *at, f32x4 v)
 {
-    const auto r = __builtin_convertvector(v, typename Element<TYPE>::four);
-    __builtin_memcpy(at, &r, sizeof r);
+    typedef typename Element<TYPE>::four Four;
+    typedef Four Anywhere __attribute__((aligned(2)));
+    const Four r = __builtin_convertvector(v, Four);
+    if (STREAM) __builtin_nontemporal_store(r, (Anywhere *)at);
+    else __builtin_memcpy(at, &r, sizeof r);
 }
 
 // Sum over each aligned run of LANES lanes (a power of two up to 64), in all of its lanes: inside sixteen lanes

@@ -52,8 +52,14 @@ FORWARD = [
     (17, 513, 0, 0, F32, BF16, 0.6, 0), (9, 770, 2, 2, F16, F16, None, 1), (11, 1024, 0, 0, F32, BF16, None, 0),
     (10, 1025, 0, 0, F32, F32, 0.5, 1), (9, 2047, 0, 0, BF16, BF16, None, 0), (12, 2048, 0, 0, F32, BF16, 0.5, 0),
     (7, 2144, 0, 0, F32, F32, None, 0), (6, 2900, 4, 0, F32, F16, 0.5, 0), (5, 4096, 0, 0, F32, F32, None, 0),
-    (5, 4097, 0, 0, BF16, F32, 0.5, 1), (4, 8192, 0, 0, F32, BF16, None, 0), (3, 10001, 0, 0, F16, F16, None, 0),
-    (3, 12289, 1, 0, F32, F32, 0.7, 0), (5, 16384, 0, 0, BF16, BF16, 0.5, 0), (2, 16383, 0, 0, F32, F32, None, 3),
+    (5, 4097, 0, 0, BF16, F32, 0.5, 1), (4, 8192, 0, 0, F32, BF16, None, 0), (3, 6001, 0, 0, F16, F16, None, 0),
+    (3, 7289, 1, 0, F32, F32, 0.7, 0), (5, 8192, 0, 0, BF16, BF16, 0.5, 0), (2, 8191, 0, 0, F32, F32, None, 3),
+    # the narrowest and widest rows of every form that the others leave out
+    (70, 4, 0, 0, F32, BF16, 0.5, 0), (70, 4, 1, 3, BF16, F16, None, 1), (900, 1, 0, 0, F16, F32, 0.5, 0),
+    (35, 66, 0, 0, F32, F32, 0.5, 1), (35, 63, 3, 0, F16, F32, None, 0), (29, 130, 0, 0, BF16, BF16, 0.5, 0),
+    (13, 257, 0, 0, F32, BF16, None, 1), (13, 259, 0, 0, F16, F16, 0.5, 0), (13, 516, 0, 0, F32, F32, None, 0),
+    (13, 768, 0, 0, BF16, BF16, 0.5, 0), (13, 769, 1, 0, F32, F32, None, 1), (7, 2049, 0, 1, F32, F32, 0.5, 0),
+    (7, 3070, 0, 0, BF16, BF16, None, 1), (7, 3073, 0, 0, F32, F16, 0.5, 0), (5, 4098, 2, 0, F16, BF16, None, 0),
 ]
 
 
@@ -130,13 +136,11 @@ def test_in_place(B):
         assert torch.equal(x, want)
 
 
-def _turns(rows, width):
-    """Rows one lane adds up: those of its workgroup's turns."""
-    pieces = -(-width // 4)
-    at_once = 32 if pieces <= 32 else 16 if pieces <= 64 else 8 if pieces <= 128 else 4 if pieces <= 256 else 1
-    turns = -(-rows // at_once)
-    groups = max(1, min(1024, -(-turns // 4)))
-    return -(-turns // groups)
+def _turns(B, rows, width):
+    """Rows one lane adds up, at most: those of its workgroup, of which a workgroup of rows of up to 1024
+    elements has at least four side by side."""
+    groups = B.tabx_layer_norm_workspace(rows, width) // (8 * width)
+    return -(-rows // groups) + 64
 
 
 # (rows, width, pad, type of x, type of the gradients, share, input's gradient, weight's, bias's)
@@ -154,8 +158,14 @@ BACKWARD = [
     (65, 1500, 0, F32, BF16, None, False, True, True), (57, 2048, 0, F32, BF16, None, True, True, True),
     (33, 2144, 0, F32, F32, 0.5, True, True, True), (21, 4001, 1, BF16, BF16, None, True, True, True),
     (14, 4100, 0, F32, F32, None, True, True, True), (9, 8192, 0, BF16, BF16, 0.5, True, True, True),
-    (5, 9001, 0, F32, F32, None, False, True, True), (7, 16384, 0, F16, F16, None, True, True, True),
-    (4, 16383, 3, F32, F32, 0.5, True, True, True),
+    (5, 7001, 0, F32, F32, None, False, True, True), (7, 8192, 0, F16, F16, None, True, True, True),
+    (4, 8191, 3, F32, F32, 0.5, True, True, True), (300, 4, 0, F32, BF16, 0.5, True, True, True),
+    (77, 4, 1, BF16, F32, None, False, True, True), (70, 66, 0, F32, F32, 0.5, True, True, True),
+    (70, 131, 0, F16, F16, None, True, True, True), (30, 257, 1, F32, BF16, 0.5, True, True, True),
+    (30, 260, 0, BF16, BF16, None, False, True, True), (30, 769, 0, F32, F32, 0.5, True, True, True),
+    (9, 1026, 0, BF16, F32, None, True, True, True), (9, 2049, 0, F32, F32, 0.5, False, True, True),
+    (9, 2050, 0, F16, F16, None, True, True, True), (9, 3074, 3, F32, BF16, None, True, True, True),
+    (9, 4099, 0, F32, F32, 0.5, True, True, True),
 ]
 
 
@@ -177,7 +187,7 @@ def test_backward(B, rows, width, pad, tx, tg, share, inputs, weights, biases):
     B.tabx_layer_norm_backward(x, weight, mean, rstd, gy, gx if inputs else None, gw, gb, ws[:size], mask)
     on = np.ones(rows, bool) if mask is None else mask.cpu().numpy() != 0
     wx, ww, wb, bx, bw, bb = R.norm_grad(R.f64(x), on, None if weight is None else R.f64(weight), R.f64(mean), R.f64(rstd),
-                                         R.f64(gy), tx, _turns(rows, width))
+                                         R.f64(gy), tx, _turns(B, rows, width))
     if inputs:
         R.near(gx, wx, bx, "grad_x")
         _outside(whole, gx)

@@ -48,7 +48,7 @@ def test_layer_norm_arguments(B):
         assert _norm(B, **kw) == -3, kw
 
 
-B_MAX = 16384
+B_MAX = 8192
 
 
 def _grad(B, rows=64, width=8, grad_x=0, gw=FAKE, gb=FAKE, ws=FAKE, size=None, mean=FAKE, rstd=FAKE, gy=None):
@@ -149,7 +149,7 @@ def test_tensors_are_checked_before_their_addresses_are_taken(B):
     refused("not one of", norm, x, w, w, 1e-5, y.to(torch.int32))
     refused("no dimensions", norm, torch.zeros(()), w, w, 1e-5, y)
     refused("rows of 15", norm, x, w, w, 1e-5, y[:, :15])
-    refused("5 rows", norm, x, w, w, 1e-5, y[:5])
+    refused("y has 5 rows", norm, x, w, w, 1e-5, y[:5])
     refused("next to each other", norm, torch.zeros(16, 6).t(), w, w, 1e-5, y)
     refused("overlap", norm, torch.zeros(1, 16).expand(6, 16), w, w, 1e-5, y)
     refused("equal distances", norm, torch.zeros(3, 4, 16)[:, :2], w, w, 1e-5, y)
