@@ -28,3 +28,11 @@ def test_no_scratch_memory_and_no_spills(listing):
     assert not re.search(r"\bscratch_(load|store)", listing)
     assert not re.search(r"\bflat_(load|store)", listing)       # every address is known to be global memory
     assert not re.search(r"\bv_pk_(add|mul|fma)_f32\b", listing)
+
+
+def test_one_lane_per_row_needs_no_lds(listing):
+    """What a lane holds of its row stays in registers (an array that is indexed by a runtime value
+    is moved to LDS without a word)."""
+    sizes = re.findall(r"\.amdhsa_kernel (_ZN4tabx\w+)\n\s+\.amdhsa_group_segment_fixed_size (\d+)", listing)
+    rows = [(n, int(s)) for n, s in sizes if "sample_actions" in n or "log_prob" in n]
+    assert len(rows) == 4 and all(s == 0 for _, s in rows), rows
