@@ -205,16 +205,17 @@ static ChoiceArgs choice_args(int64_t rows, const TabxRows *logits, const uint8_
     return a;
 }
 
+// Of one table for all, every workgroup works out the whole of it for its share of the envs.
 template <int THREADS, int ITEMS, bool EACH>
-static int launch_levels(const LevelArgs &a, void *stream)
+static int launch_levels(LevelArgs a, void *stream)
 {
     const size_t lds = sizeof(uint64_t) * THREADS * (EACH ? ITEMS : ITEMS / 4);
-    const int64_t groups = a.stride != 0 ? a.envs : ((int64_t)a.envs + THREADS - 1) / THREADS;
-    const unsigned across = (unsigned)(groups < 65536 ? groups : 65536);
+    a.share = (int32_t)least(quotient_up(quotient_up(a.envs, kComputeUnits), 64) * 64, THREADS);
+    const int64_t groups = a.stride != 0 ? a.envs : quotient_up(a.envs, a.share);
+    const unsigned across = (unsigned)least(groups, 65536);
     void *args[] = {(void *)&a};
     return launched(hipLaunchKernel((const void *)tabx_sample_levels_kernel<THREADS, ITEMS, EACH>,
-                                    dim3(across, (unsigned)((groups + across - 1) / across)), dim3(THREADS), args, lds,
-                                    (hipStream_t)stream));
+                                    dim3(across, (unsigned)quotient_up(groups, across)), dim3(THREADS), args, lds, (hipStream_t)stream));
 }
 
 } // namespace tabx
@@ -322,11 +323,15 @@ int tabx_sample_levels(int64_t envs, int32_t num_levels, const TabxRows *scores,
     a.uniform = uniform;
     a.next_level = next_level;
     a.envs = (int32_t)envs, a.levels = num_levels;
-    a.inv_temperature = 1.0 / (double)sampling->temperature;
+    a.log2e_by_temperature = 1.4426950408889634074 / (double)sampling->temperature;
+    a.reach = 44.0f * sampling->temperature;
     int bits = 0;                                  // levels <= 2^bits, so that their weights sum to at most 2^62
     while (num_levels > 1 << bits) ++bits;
-    a.scale = 62 - bits;
+    a.scale = (int32_t)least(62 - bits, 51);
+    // one table for all is read by few workgroups, each as fast as it can; one per env by many, which cover each other's waits
     if (num_levels <= 1024) return launch_levels<256, 4, true>(a, stream);
+    if (a.stride != 0 && num_levels <= 2048) return launch_levels<256, 8, true>(a, stream);
+    if (a.stride != 0 && num_levels <= 4096) return launch_levels<256, 16, true>(a, stream);
     if (num_levels <= 4096) return launch_levels<1024, 4, true>(a, stream);
     if (num_levels <= 8192) return launch_levels<1024, 8, false>(a, stream);
     return launch_levels<1024, 16, false>(a, stream);

@@ -227,6 +227,12 @@ LEVELS = [
     (30, 5000, 1, F32, "odd", True, True, 0.0, 5, 0.5, 0.0), (64, 300, None, F32, "normal", True, True, 1e-30, 0, 0.9, 0.0),
     (64, 300, None, F32, "wide", True, True, 1e30, 0, 0.9, 0.0), (400, 600, None, F32, "normal", True, True, 1.0, 600, 1.0, 0.0),
     (400, 600, None, F32, "normal", True, True, 1.0, 2 ** 31 - 1, 1e-7, 0.0),
+    (300, 1000, None, F32, "cluster", True, True, 30.0, 500, 1.0, 0.0), (300, 4096, None, F32, "cluster", False, True, 30.0, 0, 0.7, 0.0),
+    (300, 4000, None, F32, "cluster", True, True, 1.0, 3, 0.9, 0.0), (300, 8000, None, F16, "cluster", True, True, 20.0, 4000, 0.6, 0.0),
+    (300, 16000, None, F32, "cluster", True, True, 30.0, 7000, 0.8, 1e-3), (9, 4096, 1, F32, "cluster", True, True, 30.0, 2222, 0.8, 0.0),
+    (7, 3000, 0, BF16, "coarse", True, True, 1.0, 700, 0.6, 0.0), (7, 1500, 0, F32, "normal", True, True, 1.0, 700, 0.6, 0.0),
+    (66000, 300, None, F32, "normal", True, True, 1.0, 70, 0.6, 0.0), (20, 1024, 0, F32, "equal", False, False, 1.0, 300, 0.5, 0.0),
+    (300, 2000, None, F32, "normal", True, True, 0.001, 1500, 0.9999, 0.0),
 ]
 
 
@@ -242,6 +248,9 @@ def test_levels(B, envs, levels, pad, dtype, kind, lmask, emask, temperature, to
         v[:] = -2.0
     elif kind == "wide":
         v *= 20.0
+    elif kind == "cluster":                    # nearly all levels within a sliver of the scores' range
+        v *= 1e-3
+        v[:, :: max(1, levels // 3)] += 50.0
     elif kind == "odd":
         at = rng.random(v.shape)
         v[at < 0.1] = -INF
