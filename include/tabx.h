@@ -453,7 +453,7 @@ int64_t tabx_layer_norm_workspace(int64_t rows, int32_t width);
  * among those equal to it.
  * temperature 0 or in [1e-30, 1e30], top_k >= 0, 0 < top_p <= 1, 0 <= min_p <= 1 (TABX_ERR_PARAM). */
 typedef struct TabxSampling {
-    float    temperature;
+    double   temperature;
     int32_t  top_k;
     float    top_p;
     float    min_p;
@@ -491,7 +491,7 @@ int tabx_sample_levels(int64_t envs, int32_t num_levels, const TabxRows *scores,
  * [rows] f32; other rows are not written; a row without any allowed choice has 0 in both.
  * 1e-30 <= temperature <= 1e30 (TABX_ERR_PARAM). */
 int tabx_action_log_prob(int64_t rows, const TabxRows *logits, const uint8_t *action_mask,
-                         const uint8_t *controlled, const uint8_t *actions, float temperature,
+                         const uint8_t *controlled, const uint8_t *actions, double temperature,
                          float *log_prob, float *entropy, void *stream);
 
 /* The gradient of both with respect to the logits:
@@ -502,7 +502,7 @@ int tabx_action_log_prob(int64_t rows, const TabxRows *logits, const uint8_t *ac
  * grad_logits between its rows are not written.  grad_logits may be `logits` itself. */
 int tabx_action_log_prob_backward(int64_t rows, const TabxRows *logits, const uint8_t *action_mask,
                                   const uint8_t *controlled, const uint8_t *actions,
-                                  float temperature, const float *grad_log_prob,
+                                  double temperature, const float *grad_log_prob,
                                   const float *grad_entropy, const TabxRows *grad_logits,
                                   void *stream);
 

@@ -87,7 +87,7 @@ class TabxRows(C.Structure):
 class TabxSampling(C.Structure):
     """How a choice is drawn: temperature (0: the largest score), top_k (0: all), top_p (1: all),
     min_p (0: all)."""
-    _fields_ = [("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float),
+    _fields_ = [("temperature", C.c_double), ("top_k", C.c_int32), ("top_p", C.c_float),
                 ("min_p", C.c_float)]
 
     def __init__(self, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
@@ -115,14 +115,15 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.tabx_scripted_step_observe.argtypes = lib.tabx_policy_step_observe.argtypes
     lib.tabx_strerror.argtypes = [C.c_int]
     lib.tabx_strerror.restype = C.c_char_p
-    R, W, I64, I32, F32 = C.POINTER(TabxRows), C.POINTER(TabxSampling), C.c_int64, C.c_int32, C.c_float
+    R, W, I64, I32 = C.POINTER(TabxRows), C.POINTER(TabxSampling), C.c_int64, C.c_int32
+    F32, F64 = C.c_float, C.c_double
     lib.tabx_layer_norm.argtypes = [I64, I32, R, V, V, V, F32, R, V, V, V]
     lib.tabx_layer_norm_backward.argtypes = [I64, I32, R, V, V, V, V, R, R, V, V, V, I64, V]
     lib.tabx_layer_norm_workspace.argtypes = [I64, I32]
     lib.tabx_sample_actions.argtypes = [I64, R, V, V, W, V, V, V, V]
     lib.tabx_sample_levels.argtypes = [I64, I32, R, V, V, W, V, V, V]
-    lib.tabx_action_log_prob.argtypes = [I64, R, V, V, V, F32, V, V, V]
-    lib.tabx_action_log_prob_backward.argtypes = [I64, R, V, V, V, F32, V, V, R, V]
+    lib.tabx_action_log_prob.argtypes = [I64, R, V, V, V, F64, V, V, V]
+    lib.tabx_action_log_prob_backward.argtypes = [I64, R, V, V, V, F64, V, V, R, V]
     for name in EXPORTS[:-1]:
         getattr(lib, name).restype = C.c_int
     lib.tabx_layer_norm_workspace.restype = I64
@@ -268,7 +269,7 @@ TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
 # What a call on a few thousand rows costs is the time until it is enqueued: the checks are plain
-# functions of few steps (a small tabx_sample_actions takes the host 6.0 us, 10.0 as methods of an
+# functions of few steps (a small tabx_sample_actions takes the host 6.3 us, 10.1 as methods of an
 # object with torch.cuda.current_stream()).  `device` is that of a call's first tensor, -1 the host.
 
 

@@ -40,12 +40,12 @@ static int check_floats(const void *p, bool optional)
     return on_boundary(p, 4) ? TABX_OK : TABX_ERR_ALIGN;
 }
 
-static bool usable_temperature(float t) { return t >= 1e-30f && t <= 1e30f; }
+static bool usable_temperature(double t) { return t >= 1e-30 && t <= 1e30; }
 
 static int check_sampling(const TabxSampling *s)
 {
     if (!s) return TABX_ERR_NULL;
-    if (s->temperature != 0.0f && !usable_temperature(s->temperature)) return TABX_ERR_PARAM;
+    if (s->temperature != 0.0 && !usable_temperature(s->temperature)) return TABX_ERR_PARAM;
     if (s->top_k < 0 || !(s->top_p > 0.0f && s->top_p <= 1.0f) || !(s->min_p >= 0.0f && s->min_p <= 1.0f)) return TABX_ERR_PARAM;
     return TABX_OK;
 }
@@ -189,7 +189,7 @@ static int check_choices(int64_t rows, const TabxRows *logits)
 }
 
 static ChoiceArgs choice_args(int64_t rows, const TabxRows *logits, const uint8_t *action_mask, const uint8_t *controlled,
-                              float temperature)
+                              double temperature)
 {
     ChoiceArgs a = {};
     a.logits = logits->data;
@@ -199,7 +199,7 @@ static ChoiceArgs choice_args(int64_t rows, const TabxRows *logits, const uint8_
     a.controlled = controlled;
     a.rows = rows;
     a.how.temperature = temperature;
-    a.inv_temperature64 = 1.0 / (double)temperature;
+    a.inv_temperature64 = 1.0 / temperature;
     a.inv_temperature = (float)a.inv_temperature64;
     a.log2e_by_temperature = (float)(1.4426950408889634 * a.inv_temperature64);
     return a;
@@ -323,8 +323,8 @@ int tabx_sample_levels(int64_t envs, int32_t num_levels, const TabxRows *scores,
     a.uniform = uniform;
     a.next_level = next_level;
     a.envs = (int32_t)envs, a.levels = num_levels;
-    a.log2e_by_temperature = 1.4426950408889634074 / (double)sampling->temperature;
-    a.reach = 44.0f * sampling->temperature;
+    a.log2e_by_temperature = 1.4426950408889634074 / sampling->temperature;
+    a.reach = (float)(44.0 * sampling->temperature);
     int bits = 0;                                  // levels <= 2^bits, so that their weights sum to at most 2^62
     while (num_levels > 1 << bits) ++bits;
     a.scale = (int32_t)least(62 - bits, 51);
@@ -338,7 +338,7 @@ int tabx_sample_levels(int64_t envs, int32_t num_levels, const TabxRows *scores,
 }
 
 int tabx_action_log_prob(int64_t rows, const TabxRows *logits, const uint8_t *action_mask, const uint8_t *controlled,
-                         const uint8_t *actions, float temperature, float *log_prob, float *entropy, void *stream)
+                         const uint8_t *actions, double temperature, float *log_prob, float *entropy, void *stream)
 {
     using namespace tabx;
     if (!usable_temperature(temperature)) return TABX_ERR_PARAM;
@@ -354,7 +354,7 @@ int tabx_action_log_prob(int64_t rows, const TabxRows *logits, const uint8_t *ac
 }
 
 int tabx_action_log_prob_backward(int64_t rows, const TabxRows *logits, const uint8_t *action_mask, const uint8_t *controlled,
-                                  const uint8_t *actions, float temperature, const float *grad_log_prob,
+                                  const uint8_t *actions, double temperature, const float *grad_log_prob,
                                   const float *grad_entropy, const TabxRows *grad_logits, void *stream)
 {
     using namespace tabx;

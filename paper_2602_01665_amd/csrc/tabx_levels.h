@@ -378,7 +378,7 @@ __global__ __launch_bounds__(THREADS) void tabx_sample_levels_kernel(const Level
     if (most == 0) return;                         // nothing to draw from: every env keeps what it has
     const float top = score_of(most);
 
-    if (a.how.temperature == 0.0f) {
+    if (a.how.temperature == 0.0) {
         uint32_t rank = 0, none = 0;               // the lowest index counts most
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {

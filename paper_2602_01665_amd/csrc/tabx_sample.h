@@ -254,7 +254,7 @@ __global__ __launch_bounds__(256) void tabx_sample_actions_kernel(const ChoiceAr
         const Scores s = load_scores(a, r);
         int choice = TABX_ACT_NOOP;
         float log_prob = 0.0f;
-        if (a.how.temperature == 0.0f) {
+        if (a.how.temperature == 0.0) {
 #pragma unroll
             for (int i = kChoices - 1; i >= 0; --i) choice = s.l[i] == s.top ? i : choice;
             choice = s.top > -INFINITY ? choice : TABX_ACT_NOOP;

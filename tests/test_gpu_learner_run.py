@@ -108,7 +108,7 @@ def test_rollout_and_update(B):
         want = before.view(-1).cpu().numpy().copy()
         rows = R.allowed(R.f64(logits), mask.view(-1).cpu().numpy())
         for r in np.nonzero(on.cpu().numpy())[0]:
-            c = R.choose(rows[r], float(np.float32(0.9)), 6, 0.95, 0.01, float(u[r]))
+            c = R.choose(rows[r], 0.9, 6, 0.95, 0.01, float(u[r]))
             want[r] = 0 if c is None else c
         assert np.array_equal(actions.view(-1).cpu().numpy(), want), t
         kept = (x.clone(), mask, actions.view(-1).clone())

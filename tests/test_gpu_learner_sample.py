@@ -90,11 +90,10 @@ def test_actions(B, rows, pad, dtype, offset, kind, mask, share, temperature, to
     assert np.array_equal(alone.cpu().numpy(), got[:rows])
     assert torch.equal(whole.view(torch.uint8), kept.view(torch.uint8))
     l = R.allowed(R.f64(logits), am)
-    t32 = float(np.float32(temperature))
     want = np.full(rows, 99)
     for r in range(rows):
         if on is None or on[r]:
-            c = R.choose(l[r], t32, top_k, top_p, min_p, u[r])
+            c = R.choose(l[r], temperature, top_k, top_p, min_p, u[r])
             want[r] = 0 if c is None else c
     bad = np.nonzero(got[:rows] != want)[0]
     assert bad.size == 0, (bad[:5], l[bad[:3]], u[bad[:3]], got[bad[:3]], want[bad[:3]])
@@ -103,7 +102,7 @@ def test_actions(B, rows, pad, dtype, offset, kind, mask, share, temperature, to
         assert (lp.cpu().numpy()[:rows][sel] == 0).all()
     else:
         some = np.minimum(want, 7)
-        w_lp, _, b_lp, _ = R.log_prob(l, some, t32)
+        w_lp, _, b_lp, _ = R.log_prob(l, some, temperature)
         R.near(R.f64(lp)[:rows][sel], w_lp[sel], b_lp[sel], "log_prob")
     assert bool((lp.cpu()[:rows][~torch.from_numpy(sel)] == 99).all())
 
@@ -149,8 +148,8 @@ def test_log_prob_and_gradient(B, rows, pad, dtype, offset, kind, mask, share, t
     B.tabx_action_log_prob(logits, dev(acts), temperature, lp2, None, dev(am), dev(on))
     assert torch.equal(lp, lp2)
     sel = np.ones(rows, bool) if on is None else on != 0
-    l, t32 = R.allowed(R.f64(logits), am), float(np.float32(temperature))
-    w_lp, w_h, b_lp, b_h = R.log_prob(l, acts, t32)
+    l = R.allowed(R.f64(logits), am)
+    w_lp, w_h, b_lp, b_h = R.log_prob(l, acts, temperature)
     R.near(R.f64(lp)[sel], w_lp[sel], b_lp[sel], "log_prob")
     R.near(R.f64(h)[sel], w_h[sel], b_h[sel], "entropy")
     assert (R.f64(lp)[~sel] == 99).all() and (R.f64(h)[~sel] == 99).all()
@@ -159,7 +158,7 @@ def test_log_prob_and_gradient(B, rows, pad, dtype, offset, kind, mask, share, t
         out, view = _logits(rng, rows, pad, dtype, "normal", offset)
         B.tabx_action_log_prob_backward(logits, dev(acts), temperature, dev(gl) if kind_of != "entropy" else None,
                                         dev(ge) if kind_of != "log_prob" else None, view, dev(am), dev(on))
-        w_g, b_g = R.log_prob_grad(l, acts, t32, a.astype(np.float64), b.astype(np.float64), dtype)
+        w_g, b_g = R.log_prob_grad(l, acts, temperature, a.astype(np.float64), b.astype(np.float64), dtype)
         R.near(R.f64(view)[sel], w_g[sel], b_g[sel], "grad_logits " + kind_of)
         assert (R.f64(view)[~sel] == 0).all()
         left = torch.ones_like(out, dtype=torch.bool)
@@ -274,11 +273,10 @@ def test_levels(B, envs, levels, pad, dtype, kind, lmask, emask, temperature, to
     l[np.isnan(l)] = -INF
     if lm is not None:
         l[:, lm == 0] = -INF
-    t32 = float(np.float32(temperature))
     want = np.full(envs, -5)
     for e in range(envs):
         if em is None or em[e]:
-            c = R.choose(l[0 if pad is None else e], t32, top_k, top_p, min_p, u[e])
+            c = R.choose(l[0 if pad is None else e], temperature, top_k, top_p, min_p, u[e])
             want[e] = -5 if c is None else c
     bad = np.nonzero(got[:envs] != want)[0]
     assert bad.size == 0, (bad.size, bad[:5], u[bad[:5]], got[bad[:5]], want[bad[:5]])
