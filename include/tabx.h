@@ -386,7 +386,7 @@ int tabx_row_form(const TabxParams *params, int call, TabxRowForm *form);
  * These calls work on `rows` rows of the caller's own arrays, whatever they stand for: the E * N
  * units of a batch, some ticks of it, a part, the E envs.  Stream rules and errors are those of the
  * other calls; the device that owns `stream` and the arrays has to be the current one.  rows == 0
- * is a no-op that needs no arrays.  rows may not exceed 2^40, nor rows times a stride 2^62
+ * is a no-op that needs no arrays.  rows may not exceed 2^40, nor rows times a stride 2^60
  * (TABX_ERR_SHAPE).  Outputs must not overlap inputs or each other, except where it is said.
  * ------------------------------------------------------------------------------------------- */
 

@@ -421,6 +421,8 @@ def tabx_sample_levels(scores, sampling, uniform, next_level, level_mask=None, e
                        stream=None):
     """Draws each env's next level from scores [levels] of all envs or [envs, levels] of each."""
     what, u8, dev = "tabx_sample_levels", torch.uint8, scores.get_device()
+    if next_level is None:
+        _refuse(what, "next_level is needed")
     envs, n = next_level.numel(), scores.dim()
     if n > 2:
         _refuse(what, f"scores has {n} dimensions")

@@ -29,7 +29,7 @@ static int check_array(const TabxRows *m, int64_t rows, int32_t width, bool opti
 {
     if (!m) return optional ? TABX_OK : TABX_ERR_NULL;
     if (m->type < TABX_F32 || m->type > TABX_F16) return TABX_ERR_SHAPE;
-    if (m->stride < width || (rows > 0 && m->stride > ((int64_t)1 << 62) / rows)) return TABX_ERR_SHAPE;
+    if (m->stride < width || (rows > 0 && m->stride > ((int64_t)1 << 60) / rows)) return TABX_ERR_SHAPE;
     if (!m->data) return TABX_ERR_NULL;
     return on_boundary(m->data, m->type == TABX_F32 ? 4 : 2) ? TABX_OK : TABX_ERR_ALIGN;
 }
@@ -94,7 +94,7 @@ static int for_width(int pieces, const Args &...args)
             if (pieces <= LANES * (PIECES - 1)) return TABX_ERR_SHAPE;                  \
             return F<LANES, PIECES>::go(args...);                                       \
         }
-    TABX_FORM(1, 1)
+    TABX_FORM(1, 1) TABX_FORM(4, 1) TABX_FORM(8, 1)
     TABX_FORM(16, 1) TABX_FORM(16, 2) TABX_FORM(16, 3) TABX_FORM(32, 2) TABX_FORM(32, 3)
     TABX_FORM(64, 2) TABX_FORM(64, 3) TABX_FORM(64, 4) TABX_FORM(128, 3)
     TABX_FORM(256, 2) TABX_FORM(256, 3) TABX_FORM(256, 4) TABX_FORM(1024, 2)

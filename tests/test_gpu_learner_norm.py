@@ -58,6 +58,8 @@ FORWARD = [
     (70, 4, 0, 0, F32, BF16, 0.5, 0), (70, 4, 1, 3, BF16, F16, None, 1), (900, 1, 0, 0, F16, F32, 0.5, 0),
     (35, 66, 0, 0, F32, F32, 0.5, 1), (35, 63, 3, 0, F16, F32, None, 0), (29, 130, 0, 0, BF16, BF16, 0.5, 0),
     (13, 257, 0, 0, F32, BF16, None, 1), (13, 259, 0, 0, F16, F16, 0.5, 0), (13, 516, 0, 0, F32, F32, None, 0),
+    (300, 8, 0, 0, F32, F32, 0.5, 0), (301, 16, 0, 0, BF16, BF16, None, 0), (90, 17, 0, 0, F32, BF16, 0.5, 1),
+    (500, 14, 3, 1, F16, F32, 0.5, 0), (200, 30, 0, 0, F32, F32, 0.5, 0), (77, 36, 0, 0, BF16, F32, None, 0),
     (13, 768, 0, 0, BF16, BF16, 0.5, 0), (13, 769, 1, 0, F32, F32, None, 1), (7, 2049, 0, 1, F32, F32, 0.5, 0),
     (7, 3070, 0, 0, BF16, BF16, None, 1), (7, 3073, 0, 0, F32, F16, 0.5, 0), (5, 4098, 2, 0, F16, BF16, None, 0),
 ]
@@ -160,7 +162,9 @@ BACKWARD = [
     (14, 4100, 0, F32, F32, None, True, True, True), (9, 8192, 0, BF16, BF16, 0.5, True, True, True),
     (5, 7001, 0, F32, F32, None, False, True, True), (7, 8192, 0, F16, F16, None, True, True, True),
     (4, 8191, 3, F32, F32, 0.5, True, True, True), (300, 4, 0, F32, BF16, 0.5, True, True, True),
-    (77, 4, 1, BF16, F32, None, False, True, True), (70, 66, 0, F32, F32, 0.5, True, True, True),
+    (77, 4, 1, BF16, F32, None, False, True, True), (3000, 16, 0, F32, F32, 0.5, True, True, True),
+    (2001, 13, 1, BF16, BF16, 0.5, True, True, True), (900, 32, 0, F32, BF16, None, False, True, True),
+    (700, 18, 0, F16, F32, 0.5, True, True, False), (70, 66, 0, F32, F32, 0.5, True, True, True),
     (70, 131, 0, F16, F16, None, True, True, True), (30, 257, 1, F32, BF16, 0.5, True, True, True),
     (30, 260, 0, BF16, BF16, None, False, True, True), (30, 769, 0, F32, F32, 0.5, True, True, True),
     (9, 1026, 0, BF16, F32, None, True, True, True), (9, 2049, 0, F32, F32, 0.5, False, True, True),
