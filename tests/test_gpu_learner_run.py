@@ -132,6 +132,46 @@ def test_rollout_and_update(B):
         assert off <= 4 * other + 64 * R.U * size, k
 
 
+def test_between_the_ends_pytorch_differentiates(B):
+    """The rows' layer norm and the log-probabilities at the ends, a network of PyTorch's between
+    them: its graph is entered with the logits' gradient and left with the rows'.  Held to 64 bits
+    as the update above."""
+    rows, width, dtype = 300, 176, torch.float32
+    g = torch.Generator(device=DEV).manual_seed(3)
+    n = lambda *s: torch.randn(*s, generator=g, device=DEV)  # noqa: E731
+    p = {"w0": 1 + 0.1 * n(width), "b0": 0.1 * n(width), "m1": n(width, 9) / width ** 0.5}
+    x, on = 3.0 * n(rows, width), (n(rows) > 0).to(torch.uint8)
+    acts = torch.randint(0, 8, (rows,), generator=g, device=DEV).to(torch.uint8)
+    adv, coef = n(rows), 0.02
+    y, mean, rstd = torch.zeros(rows, width, device=DEV), torch.zeros(rows, device=DEV), torch.zeros(rows, device=DEV)
+    B.tabx_layer_norm(x, p["w0"], p["b0"], EPS, y, mean, rstd, on)
+    y.requires_grad_()
+    m1 = p["m1"].clone().requires_grad_()
+    logits = torch.tanh(y @ m1)[:, :8]
+    grad_logits = torch.empty(rows, 8, device=DEV)
+    B.tabx_action_log_prob_backward(logits, acts, 1.0, -adv, torch.full_like(adv, -coef), grad_logits, None, on)
+    logits.backward(grad_logits)
+    got = {"m1": m1.grad, "w0": torch.empty(width, device=DEV), "b0": torch.empty(width, device=DEV)}
+    ws = torch.empty(B.tabx_layer_norm_workspace(rows, width), dtype=torch.uint8, device=DEV)
+    B.tabx_layer_norm_backward(x, p["w0"], mean, rstd, y.grad, None, got["w0"], got["b0"], ws, on)
+    want = []
+    for t in (torch.float64, torch.float32):
+        q = {k: v.detach().cpu().to(t).requires_grad_() for k, v in p.items()}
+        z = x.cpu().to(t)
+        c = z - z.mean(1, keepdim=True)
+        h = c / torch.sqrt((c * c).mean(1, keepdim=True) + EPS) * q["w0"] + q["b0"]
+        h = torch.where(on.cpu()[:, None] != 0, h, torch.zeros((), dtype=t))
+        lp = torch.log_softmax(torch.tanh(h @ q["m1"])[:, :8], 1)
+        keep = on.cpu().to(t)
+        taken = lp.gather(1, acts.cpu().long()[:, None])[:, 0]
+        ((-(adv.cpu().to(t) * taken) + coef * (lp.exp() * lp).sum(1)) * keep).sum().backward()
+        want.append({k: v.grad for k, v in q.items()})
+    for k, v in want[0].items():
+        off, other = float((got[k].cpu().double() - v).norm()), float((want[1][k].double() - v).norm())
+        assert off <= 4 * other + 64 * R.U * float(v.norm()), (k, off, other)
+    assert y.dtype is dtype
+
+
 def test_observations_of_the_learning_side_alone(B):
     """norm_obs on the environment's own rows: the other side's are left as they were."""
     env = _env(B, "c3_16384env_10v10", 50)
