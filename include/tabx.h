@@ -423,7 +423,7 @@ int tabx_layer_norm(int64_t rows, int32_t width, const TabxRows *x, const uint8_
  *   grad_x_j = rstd * (g_j - sum_j g_j / width - h_j * sum_j (g_j h_j) / width),
  *   grad_weight_j = sum over rows of grad_y_j h_j, grad_bias_j = sum over rows of grad_y_j.
  * Rows that are masked out are not read and add nothing; their grad_x is zero.  grad_x (NULL:
- * not wanted, as for an observation) may be grad_y itself.  grad_weight / grad_bias: device
+ * not wanted, as for an observation) may be grad_y itself (same data, stride and type).  grad_weight / grad_bias: device
  * [width] f32, overwritten (with zeros if there are no rows), each may be NULL.  The sums are always taken in the same order: equal
  * calls give equal bits.  `workspace`: device memory, 16-byte aligned, of at least
  * tabx_layer_norm_workspace(rows, width) bytes (TABX_ERR_SHAPE if workspace_bytes is less), needed
@@ -499,7 +499,8 @@ int tabx_action_log_prob(int64_t rows, const TabxRows *logits, const uint8_t *ac
  * for the allowed choices, zero for the others and for rows that are not controlled (these are
  * written: the gradient of logits that were not used).  grad_log_prob / grad_entropy [rows] f32,
  * each may be NULL (zero), not both; a log_prob of -infinity passes nothing back.  The elements of
- * grad_logits between its rows are not written.  grad_logits may be `logits` itself. */
+ * grad_logits between its rows are not written.  grad_logits may be `logits` itself
+ * (same data, stride and type). */
 int tabx_action_log_prob_backward(int64_t rows, const TabxRows *logits, const uint8_t *action_mask,
                                   const uint8_t *controlled, const uint8_t *actions,
                                   double temperature, const float *grad_log_prob,

@@ -183,27 +183,6 @@ __device__ __forceinline__ uint64_t level_number(uint32_t key, int j)
     return (uint64_t)key << kIndexBits | (uint32_t)((1 << kIndexBits) - 1 - j);
 }
 
-// The weights of a thread's levels: in registers, or from the scores again where there are too many of them.
-template <int THREADS, int ITEMS>
-struct Weights {
-    static constexpr bool kStored = THREADS < 1024 || ITEMS <= 8;
-    uint64_t w[kStored ? ITEMS : 1];
-    float    top;
-    __device__ __forceinline__ void take(const uint32_t (&key)[ITEMS], const LevelArgs &a)
-    {
-        if (kStored) {
-#pragma unroll
-            for (int i = 0; i < ITEMS; ++i) w[kStored ? i : 0] = level_weight(key[i], top, a);
-        }
-    }
-    __device__ __forceinline__ uint64_t of(int i, uint32_t key, const LevelArgs &a) const
-    {
-        if (kStored) return w[kStored ? i : 0];
-        __builtin_amdgcn_sched_barrier(0);         // one after the other: side by side they would not fit the registers
-        return level_weight(key, top, a);
-    }
-};
-
 // Where the bins' contents, added up in falling order of the scores, reach what is wanted.  By the first wavefront.
 // RISING: bin 0 has the largest scores.  MASS: weights count, else levels.  share < 1: wanted is that share of them all.
 template <bool RISING, bool MASS>
@@ -240,8 +219,8 @@ __device__ __forceinline__ void cross(LevelShared &sh, uint64_t want, float shar
 // The number of the level that is the last to be kept, eight bits at a time.  want: how many levels (MASS false), or the
 // weight that the levels before a kept one stay under (MASS true; > 0).  Only numbers >= floor compete.
 template <int THREADS, int ITEMS, bool MASS>
-__device__ __forceinline__ uint64_t threshold_by_bits(uint32_t (&key)[ITEMS], const Weights<THREADS, ITEMS> &weight, uint64_t floor,
-                                                      uint64_t want, const LevelArgs &a, LevelShared &sh)
+__device__ __forceinline__ uint64_t threshold_by_bits(uint32_t (&key)[ITEMS], const uint64_t (&weight)[ITEMS], uint64_t floor,
+                                                      uint64_t want, LevelShared &sh)
 {
     uint64_t prefix = 0;
     // 48 bits from the top, the two highest of them always zero
@@ -256,7 +235,7 @@ __device__ __forceinline__ uint64_t threshold_by_bits(uint32_t (&key)[ITEMS], co
             if (key[i] != 0 && c >= floor && (c >> (shift + 8)) == (prefix >> (shift + 8))) {
                 const int b = (int)(c >> shift) & 255;
                 atomicAdd(&sh.count[b], 1u);
-                if (MASS) atomicAdd((unsigned long long *)&sh.mass[b], (unsigned long long)weight.of(i, key[i], a));
+                if (MASS) atomicAdd((unsigned long long *)&sh.mass[b], (unsigned long long)weight[i]);
             }
         }
         __syncthreads();
@@ -275,7 +254,7 @@ __device__ __forceinline__ uint64_t threshold_by_bits(uint32_t (&key)[ITEMS], co
 // The same by ranges and rivals.  Of MASS, want is top_p times all that competes; without, top_k levels.  0: all are kept
 // that have a weight.
 template <int THREADS, int ITEMS, bool MASS>
-__device__ __forceinline__ uint64_t threshold(uint32_t (&key)[ITEMS], const Weights<THREADS, ITEMS> &weight, const Ranges &ranges,
+__device__ __forceinline__ uint64_t threshold(uint32_t (&key)[ITEMS], const uint64_t (&weight)[ITEMS], const Ranges &ranges,
                                               uint64_t floor, const LevelArgs &a, LevelShared &sh)
 {
     for (int b = (int)threadIdx.x; b < 256; b += THREADS) sh.count[b] = 0, sh.mass[b] = 0;
@@ -287,7 +266,7 @@ __device__ __forceinline__ uint64_t threshold(uint32_t (&key)[ITEMS], const Weig
         if (key[i] != 0 && level_number(key[i], ((i / 4) * THREADS + (int)threadIdx.x) * 4 + i % 4) >= floor) {
             const int b = ranges.of(key[i]);
             atomicAdd(&sh.count[b], 1u);
-            if (MASS) atomicAdd((unsigned long long *)&sh.mass[b], (unsigned long long)weight.of(i, key[i], a));
+            if (MASS) atomicAdd((unsigned long long *)&sh.mass[b], (unsigned long long)weight[i]);
         }
     }
     __syncthreads();
@@ -301,7 +280,7 @@ __device__ __forceinline__ uint64_t threshold(uint32_t (&key)[ITEMS], const Weig
         if (THREADS * ITEMS > 8192) asm volatile("" : "+v"(key[i]));
         const uint64_t c = level_number(key[i], ((i / 4) * THREADS + (int)threadIdx.x) * 4 + i % 4);
         if (key[i] != 0 && c >= floor && ranges.of(key[i]) == range) {
-            const uint64_t w = weight.of(i, key[i], a);
+            const uint64_t w = weight[i];
             if (w != 0) {                          // (one without is never drawn, wherever the threshold is)
                 const uint32_t at = atomicAdd(&sh.found, 1u);
                 if (at < (uint32_t)kRivals) sh.rivals[at] = Rival{c, w};
@@ -313,7 +292,7 @@ __device__ __forceinline__ uint64_t threshold(uint32_t (&key)[ITEMS], const Weig
     if (found > (uint32_t)kRivals) {
         const uint64_t all = sh.all;
         __syncthreads();
-        return threshold_by_bits<THREADS, ITEMS, MASS>(key, weight, floor, all, a, sh);
+        return threshold_by_bits<THREADS, ITEMS, MASS>(key, weight, floor, all, sh);
     }
     if (threadIdx.x < found) {
         const Rival mine = sh.rivals[threadIdx.x];
@@ -390,9 +369,9 @@ __global__ __launch_bounds__(THREADS) void tabx_sample_levels_kernel(const Level
         return;
     }
 
-    Weights<THREADS, ITEMS> weight;
-    weight.top = top;
-    weight.take(key, a);
+    uint64_t weight[ITEMS];
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) weight[i] = level_weight(key[i], top, a);
 
     const Ranges ranges(top, score_of(~low_end), a.reach);
     uint64_t floor = 0;
@@ -412,7 +391,7 @@ __global__ __launch_bounds__(THREADS) void tabx_sample_levels_kernel(const Level
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const uint64_t c = level_number(key[4 * t + q], at * 4 + q);
-            kept[q] = key[4 * t + q] != 0 && c >= floor ? weight.of(4 * t + q, key[4 * t + q], a) : 0;
+            kept[q] = key[4 * t + q] != 0 && c >= floor ? weight[4 * t + q] : 0;
             if (kept[q] < least) kept[q] = 0;
             sum += kept[q];
         }

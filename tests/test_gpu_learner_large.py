@@ -138,3 +138,53 @@ def test_levels(B):
     for s in _parts(70001, 9973):
         B.tabx_sample_levels(tables[s], B.TabxSampling(0.7, 9), u[s], parts[s])
     assert torch.equal(whole, parts)
+
+
+def test_more_rows_than_32_bits_count(B):
+    """2^31 rows and some: the last ones are worked on where they lie."""
+    rows, few = 2 ** 31 + 300, 700
+    last = slice(rows - few, rows)
+    z = torch.zeros(rows, 8, dtype=BF16, device=DEV)
+    n = _normal(9)
+    z[last] = n(few, 8).to(BF16)
+    u = torch.zeros(rows, device=DEV)
+    u[last] = torch.rand(few, device=DEV)
+    a = torch.zeros(rows, dtype=torch.uint8, device=DEV)
+    how = B.TabxSampling(0.9, 5)
+    B.tabx_sample_actions(z, how, u, a)
+    want = torch.zeros(few, dtype=torch.uint8, device=DEV)
+    B.tabx_sample_actions(z[last].clone(), how, u[last].clone(), want)
+    assert torch.equal(a[last], want)
+    del u
+    g, want = torch.ones_like(z), torch.empty(few, 8, dtype=BF16, device=DEV)
+    lp = torch.full((rows,), 0.5, device=DEV)
+    B.tabx_action_log_prob_backward(z, a, 1.0, lp, None, g)
+    B.tabx_action_log_prob_backward(z[last].clone(), a[last].clone(), 1.0, lp[:few].clone(), None, want)
+    assert torch.equal(g[last], want)
+    B.tabx_action_log_prob(z, a, 1.0, lp)
+    want = torch.empty(few, device=DEV)
+    B.tabx_action_log_prob(z[last].clone(), a[last].clone(), 1.0, want)
+    assert torch.equal(lp[last], want)
+    del z, g, a, lp
+    torch.cuda.empty_cache()
+    x = torch.zeros(rows, 5, dtype=BF16, device=DEV)
+    x[last] = n(few, 5).to(BF16)
+    w = 1.0 + n(5)
+    y, mean, rstd = torch.ones_like(x), torch.ones(rows, device=DEV), torch.ones(rows, device=DEV)
+    B.tabx_layer_norm(x, w, None, 1e-5, y, mean, rstd)
+    part = [torch.empty(few, 5, dtype=BF16, device=DEV), torch.empty(few, device=DEV), torch.empty(few, device=DEV)]
+    B.tabx_layer_norm(x[last].clone(), w, None, 1e-5, *part)
+    for p, q in zip((y, mean, rstd), part):
+        assert torch.equal(p[last], q)
+    ws = torch.empty(B.tabx_layer_norm_workspace(rows, 5), dtype=torch.uint8, device=DEV)
+    gw, gx = torch.empty(5, device=DEV), torch.ones_like(x)
+    B.tabx_layer_norm_backward(x, w, mean, rstd, y, gx, gw, None, ws)
+    want, wx = torch.empty(5, device=DEV), torch.empty(few, 5, dtype=BF16, device=DEV)
+    B.tabx_layer_norm_backward(x[last].clone(), w, *part[1:], part[0], wx, want, None, ws)
+    assert torch.equal(gx[last], wx)
+    # (the other rows are all zero and add exactly nothing)
+    h = (x[last].double() - mean[last, None].double()) * rstd[last, None].double()
+    mag = (part[0].double() * h).abs().sum(0)
+    assert bool(((gw.double() - want.double()).abs() <= 2 * (few + 64 + 64) * R.U * mag).all())
+    del x, y, mean, rstd, gx
+    torch.cuda.empty_cache()
