@@ -27,7 +27,8 @@ struct NormArgs {
     const uint8_t *row_mask;
     const float *weight, *bias;
     float      *mean, *rstd;       // forward: written; backward: read
-    float      *partial;           // backward: [workgroup][2][width]
+    float      *partial;           // backward: [workgroup][2][width], or nullptr
+    float      *grad_weight, *grad_bias;   // backward of a single workgroup, if `partial` is nullptr
     int64_t     rows, x_stride, y_stride, g_stride;
     int64_t     team_rows, lap;    // a team's rows are runs of at most 64 of them, `lap` rows from one run to the next
     int32_t     width, x_type, y_type, g_type;
@@ -374,7 +375,7 @@ __global__ __launch_bounds__(threads_of(LANES), grad_wavefronts(PIECES)) void ta
     if constexpr (INPUTS) load_columns(w, a.weight, 1.0f, cut, a.width);
 #pragma unroll
     for (int q = 0; q < PIECES; ++q) dw[q] = zero, db[q] = zero;
-    const bool sums = !INPUTS || a.partial != nullptr;
+    const bool sums = !INPUTS || a.partial || a.grad_weight || a.grad_bias;
     // a row's mean and rstd are the same for a whole wavefront; without a lane's own address they would be moved to
     // scalar registers as soon as they are loaded, and waited for
     int here = 0;
@@ -443,9 +444,12 @@ __global__ __launch_bounds__(threads_of(LANES), grad_wavefronts(PIECES)) void ta
     walk_through<kGradAhead<LANES>, Rows>(more, fetch, work);
     if (!sums) return;
     // the rows worked on side by side in a wavefront, then the wavefronts
-    float *const out = a.partial + (int64_t)blockIdx.x * 2 * a.width;
+    const int64_t part = (int64_t)blockIdx.x * 2 * a.width;
+    float *const outs[2] = {a.partial ? a.partial + part : a.grad_weight, a.partial ? a.partial + part + a.width : a.grad_bias};
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
+        float *const out = outs[half];
+        if (!out) continue;                        // (the same for all)
 #pragma unroll
         for (int q = 0; q < PIECES; ++q) {
             f32x4 v = half ? db[q] : dw[q];
@@ -465,7 +469,7 @@ __global__ __launch_bounds__(threads_of(LANES), grad_wavefronts(PIECES)) void ta
 #pragma unroll
                 for (int k = 1; k < WAVES; ++k) v += meet[LANES <= 64 ? k : 0][LANES <= 64 ? cut.lane : 0];
             }
-            float *at = out + half * a.width + cut.at(q);
+            float *at = out + cut.at(q);
             if (q < PIECES - 1) {
                 store_four<TABX_F32>(at, v);
             } else {

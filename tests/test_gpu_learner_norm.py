@@ -207,6 +207,32 @@ def test_backward(B, rows, width, pad, tx, tg, share, inputs, weights, biases):
     assert gb is None or torch.equal(gb, gb2)
 
 
+@pytest.mark.parametrize("width", [1, 3, 4, 18, 33, 96, 130, 314, 515, 1026, 2048, 4099, 8191])
+@pytest.mark.parametrize("rows", [1, 4, 8, 9])
+def test_weight_gradients_of_few_rows(B, rows, width):
+    """Each of the two alone and both, with nothing written around them, in a first and in a second call."""
+    _say("norm grad of few rows", rows, width)
+    rng = np.random.default_rng(rows * 10000 + width)
+    _, x = _rows(rng, rows, width, 1, F32, 2.0, 1.0, 1)
+    _, gy = _rows(rng, rows, width, 0, F32)
+    mean = x.mean(1).contiguous()
+    rstd = torch.rsqrt(x.var(1, unbiased=False) + 1e-5).contiguous()
+    _, ww, wb, _, bw, bb = R.norm_grad(R.f64(x), np.ones(rows, bool), None, R.f64(mean), R.f64(rstd), R.f64(gy), F32, rows + 64)
+    ws = torch.empty(B.tabx_layer_norm_workspace(rows, width), dtype=torch.uint8, device=DEV)
+    for weights, biases in ((True, True), (True, False), (False, True)):
+        whole = torch.full((2, width + 16), 7.0, device=DEV)
+        gw, gb = (whole[i, 8:8 + width] if on else None for i, on in enumerate((weights, biases)))
+        for _ in range(2):
+            B.tabx_layer_norm_backward(x, None, mean, rstd, gy, None, gw, gb, ws)
+        if weights:
+            R.near(gw, ww, bw, "grad_weight")
+        if biases:
+            R.near(gb, wb, bb, "grad_bias")
+        for i, on in enumerate((weights, biases)):
+            assert bool((whole[i, :8] == 7).all()) and bool((whole[i, 8 + width:] == 7).all())
+            assert on or bool((whole[i] == 7).all())
+
+
 def test_gradient_against_differences(B):
     """sum(gy * norm(x)) along random directions, from the forward call in float32: a central
     difference of step h is off by h^2 and by the rounding of two sums over h."""
