@@ -302,7 +302,7 @@ int tabx_sample_actions(int64_t rows, const TabxRows *logits, const uint8_t *act
     if (!actions) return TABX_ERR_NULL;
     if ((rc = check_floats(uniform, false)) || (rc = check_floats(log_prob, true))) return rc;
     ChoiceArgs a = choice_args(rows, logits, action_mask, controlled, sampling->temperature);
-    a.how = *sampling;
+    a.how = settings_of(*sampling);
     a.uniform = uniform;
     a.actions_out = actions;
     a.log_prob = log_prob;

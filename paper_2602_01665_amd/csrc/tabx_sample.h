@@ -104,14 +104,27 @@ __device__ __forceinline__ float log_of_sum(float others)
     return fmaf(others - (sum - 1.0f), __builtin_amdgcn_rcpf(sum), kLn2 * __builtin_amdgcn_logf(sum));
 }
 
-__device__ __forceinline__ float usable_uniform(float u) { return u > 0.0f ? fminf(u, 0x1.fffffep-1f) : 0.0f; }
+__host__ __device__ __forceinline__ float usable_uniform(float u) { return u > 0.0f ? fminf(u, 0x1.fffffep-1f) : 0.0f; }
 
-// The choice that `uniform` points to among the kept ones.  Every decision compares sums of weights; `nearest` becomes the
-// smallest difference that decided one.  All selects, no branches: the lanes' rows differ.
-template <bool FILTER>
-__device__ __forceinline__ int pick(const Scores &s, const float (&w)[kChoices], const TabxSampling &how, float uniform,
-                                    float &nearest)
+constexpr float kMargin = 0x1p-16f;
+
+// The same settings as the kernel takes them.  The largest weight is 1 and all together are at most kChoices: up to a top_p of
+// one by that many the second is never kept, and no comparison needs to find out.
+inline TabxSampling settings_of(TabxSampling how)
 {
+    if (how.top_p <= 1.0f / kChoices) how.top_k = 1, how.top_p = 1.0f;
+    return how;
+}
+
+// The choice that `uniform` points to among the kept ones.  Every decision compares weights or sums of them; `spare` becomes
+// the least that a difference which decided one had beyond its margin.  Two weights or sums that a filter compares are as
+// exact as they are large, and so is their margin; the draw's is that of the sum of all.  All selects, no branches: the
+// lanes' rows differ.
+template <bool FILTER>
+__host__ __device__ __forceinline__ int pick(const Scores &s, const float (&w)[kChoices], const TabxSampling &how, float uniform,
+                                             float &spare)
+{
+    spare = 1.0f;
     float kept[kChoices];
 #pragma unroll
     for (int i = 0; i < kChoices; ++i) kept[i] = w[i];
@@ -131,40 +144,42 @@ __device__ __forceinline__ int pick(const Scores &s, const float (&w)[kChoices],
         for (int i = 0; i < kChoices; ++i) kept[i] = rank[i] < how.top_k ? kept[i] : 0.0f;
     }
     if (FILTER && how.top_p < 1.0f) {
-        // the weights before it: those of lower index, but for the ones that come later
-        float ahead[kChoices], among = 0.0f;
+        // What comes before it is less than top_p of all where it and what comes after are more than the rest of all: sums
+        // of few small weights, which keep their bits where top_p is close to one.
+        float tail[kChoices], among = 0.0f;
 #pragma unroll
         for (int i = 0; i < kChoices; ++i) {
-            ahead[i] = among;
+            tail[i] = kept[i];
             among += kept[i];
         }
 #pragma unroll
         for (int i = 0; i < kChoices; ++i)
 #pragma unroll
             for (int j = i + 1; j < kChoices; ++j) {
-                const float later = s.l[j] > s.l[i] ? 1.0f : 0.0f;
-                ahead[i] = fmaf(later, kept[j], ahead[i]);
-                ahead[j] = fmaf(-later, kept[i], ahead[j]);
+                const bool later = s.l[j] > s.l[i];
+                tail[i] += later ? 0.0f : kept[j];
+                tail[j] += later ? kept[i] : 0.0f;
             }
+        const float rest = (1.0f - how.top_p) * among;
 #pragma unroll
         for (int i = 0; i < kChoices; ++i) {
-            const float over = fmaf(-how.top_p, among, ahead[i]);
-            nearest = fminf(nearest, kept[i] > 0.0f ? fabsf(over) : nearest);
-            kept[i] = over < 0.0f ? kept[i] : 0.0f;
+            const float over = tail[i] - rest;
+            spare = fminf(spare, fmaf(-kMargin, tail[i], fabsf(over)));
+            kept[i] = over > 0.0f ? kept[i] : 0.0f;
         }
     }
     if (FILTER && how.min_p > 0.0f) {
 #pragma unroll
         for (int i = 0; i < kChoices; ++i) {
             const float over = w[i] - how.min_p;
-            nearest = fminf(nearest, s.l[i] != s.top ? fabsf(over) : nearest);
+            spare = fminf(spare, s.l[i] != s.top ? fmaf(-kMargin, w[i], fabsf(over)) : spare);
             kept[i] = over >= 0.0f ? kept[i] : 0.0f;
         }
     }
     float total = 0.0f;
 #pragma unroll
     for (int i = 0; i < kChoices; ++i) total += kept[i];
-    float left = usable_uniform(uniform) * total;
+    float left = usable_uniform(uniform) * total, nearest = 1.0f;
     // the first whose running sum exceeds that: as many as do not come before it
     int choice = 0;
 #pragma unroll
@@ -173,6 +188,7 @@ __device__ __forceinline__ int pick(const Scores &s, const float (&w)[kChoices],
         nearest = fminf(nearest, fabsf(left));
         choice += left < 0.0f ? 0 : 1;
     }
+    spare = fminf(spare, nearest - kMargin);
     return choice;
 }
 
@@ -238,9 +254,15 @@ __device__ __forceinline__ int pick_exactly(const Scores &s, const TabxSampling 
 }
 
 // One lane per row.  The draw is decided in 32 bits where no comparison is closer than the weights are exact, and in 64
-// bits else (once in some thousand rows).  A sum of eight weights is off by 26 * 2^-24 from the weights and by 28 * 2^-24
-// from its own additions (seven, each of half a step below 8), the weights before one by as much again, top_p or
-// `uniform` times a sum by another 4 * 2^-24: below 200 * 2^-24 on both sides of a comparison, under the margin of 2^-16.
+// bits else.  In steps of 2^-24:
+//   - a sum of eight weights is off by 26 from the weights and by 28 from its own additions (seven, each of half a step below
+//     8), the weights before one by as much again, `uniform` times a sum by another 4: below 200 on both sides of the draw's
+//     comparison, under the margin of 256;
+//   - a weight that min_p or top_p may leave out wrongly moves these sums by itself: eight below 2^-22 by 32, still under the
+//     margin, and one above that is off by 49 of itself, a sum of it and those that come after it by 59 of itself, (1 - top_p)
+//     times the sum of all by 57 of itself: under the margin of 256 of itself.
+// A draw is so close once in some thousand rows, and so is a filter, but where the scores make ties of them: eight equal ones
+// and a top_p of one half.
 // FILTER: top_k, top_p or min_p leave something out.  655360 rows of nine f32, 28 MB: 7.7 us; 327680 of bf16, half of them
 // controlled, all filters: 7.7 us (9.3 with each lane's own 64-bit decision).  96 rows: 2.8 us, 6.8 from call to call.
 template <bool FILTER>
@@ -261,9 +283,9 @@ __global__ __launch_bounds__(256) void tabx_sample_actions_kernel(const ChoiceAr
         } else {
             const bool some = s.top > -INFINITY;
             const Weights8 w = weigh(s, a);
-            float nearest = 1.0f;
-            choice = pick<FILTER>(s, w.w, a.how, uniform, nearest);
-            for (uint64_t close = __ballot(on && some && nearest <= 0x1p-16f); close != 0; close &= close - 1) {
+            float spare;
+            choice = pick<FILTER>(s, w.w, a.how, uniform, spare);
+            for (uint64_t close = __ballot(on && some && spare <= 0.0f); close != 0; close &= close - 1) {
                 const int source = __builtin_ctzll(close);
                 const int exact = pick_exactly<FILTER>(s, a.how, uniform, a.inv_temperature64, source);
                 choice = ((int)threadIdx.x & 63) == source ? exact : choice;
