@@ -192,43 +192,46 @@ __host__ __device__ __forceinline__ int pick(const Scores &s, const float (&w)[k
     return choice;
 }
 
-__device__ __forceinline__ float from_lane(float v, int lane)
+// v of another lane.
+__device__ __forceinline__ float of_lane(float v, int lane)
 {
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+    return __int_as_float(__builtin_amdgcn_ds_bpermute(lane * 4, __float_as_int(v)));
 }
 
-__device__ __forceinline__ double from_lane(double v, int lane)
+// v of lane I of each eight.
+template <int I>
+__device__ __forceinline__ double of_eight(double v)
 {
     const uint64_t b = (uint64_t)__double_as_longlong(v);
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, lane);
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_ds_swizzle((int)(uint32_t)b, I << 5 | 0x18);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_ds_swizzle((int)(uint32_t)(b >> 32), I << 5 | 0x18);
     return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
 }
 
-// The same in 64 bits for the row of lane `source`, by the whole wavefront: lane j has choice j mod 8.  (Each lane for its
-// own row, the few wavefronts that need it would be the last to finish, a thousand instructions after the others.)
+// The same in 64 bits for the row of lane `source`, by the eight lanes it is one of: lane j has choice j mod 8.  (Each lane for
+// its own row, the few wavefronts that need it would be the last to finish, a thousand instructions after the others.
+// 327680 rows: 9.3 us.)
 template <bool FILTER>
 __device__ __forceinline__ int pick_exactly(const Scores &s, const TabxSampling &how, float uniform, double inv_temperature,
                                             int source)
 {
-    const int j = (int)threadIdx.x & 7;
-    const float top = from_lane(s.top, source);
+    const int j = (int)threadIdx.x & 7, eight = (int)threadIdx.x & 56;
+    const float top = of_lane(s.top, source);
     float l[kChoices], mine;
 #pragma unroll
     for (int i = 0; i < kChoices; ++i) {
-        l[i] = from_lane(s.l[i], source);
+        l[i] = of_lane(s.l[i], source);
         mine = i == 0 || j == i ? l[i] : mine;
     }
     const double own = exp(((double)mine - (double)top) * inv_temperature);
-    double w[kChoices];
-#pragma unroll
-    for (int i = 0; i < kChoices; ++i) w[i] = from_lane(own, i);
+    double w[kChoices] = {of_eight<0>(own), of_eight<1>(own), of_eight<2>(own), of_eight<3>(own),
+                          of_eight<4>(own), of_eight<5>(own), of_eight<6>(own), of_eight<7>(own)};
     if constexpr (FILTER) {
         uint32_t ahead = 0;                        // which come before it
 #pragma unroll
         for (int i = 0; i < kChoices; ++i) ahead |= l[i] > mine || (i < j && l[i] == mine) ? 1u << i : 0u;
         const bool few = how.top_k == 0 || __builtin_popcount(ahead) < how.top_k;
-        const uint32_t among = (uint32_t)__ballot(few);
+        const uint32_t among = (uint32_t)(__ballot(few) >> eight);
         double before = 0.0, most = 0.0;
 #pragma unroll
         for (int i = 0; i < kChoices; ++i) {
@@ -236,14 +239,14 @@ __device__ __forceinline__ int pick_exactly(const Scores &s, const TabxSampling 
             most += among >> i & 1 ? w[i] : 0.0;
         }
         const bool enough = how.top_p >= 1.0f || before < (double)how.top_p * most;
-        const uint32_t kept = (uint32_t)__ballot(few && enough && own >= (double)how.min_p);
+        const uint32_t kept = (uint32_t)(__ballot(few && enough && own >= (double)how.min_p) >> eight);
 #pragma unroll
         for (int i = 0; i < kChoices; ++i) w[i] = kept >> i & 1 ? w[i] : 0.0;
     }
     double at = 0.0, upto = 0.0;
 #pragma unroll
     for (int i = 0; i < kChoices; ++i) at += w[i];
-    at *= (double)usable_uniform(from_lane(uniform, source));
+    at *= (double)usable_uniform(of_lane(uniform, source));
     int choice = 0;
 #pragma unroll
     for (int i = 0; i < kChoices; ++i) {
@@ -262,11 +265,13 @@ __device__ __forceinline__ int pick_exactly(const Scores &s, const TabxSampling 
 //     margin, and one above that is off by 49 of itself, a sum of it and those that come after it by 59 of itself, (1 - top_p)
 //     times the sum of all by 57 of itself: under the margin of 256 of itself.
 // A draw is so close once in some thousand rows, and so is a filter, but where the scores make ties of them: eight equal ones
-// and a top_p of one half.
+// and a top_p of one half send every row to the 64 bits, one of each eight lanes' at a time (655360 rows 37 us; 235 with one
+// of the wavefront's).
 // FILTER: top_k, top_p or min_p leave something out.  655360 rows of nine f32, 28 MB: 7.7 us; 327680 of bf16, half of them
-// controlled, all filters: 7.7 us (9.3 with each lane's own 64-bit decision).  96 rows: 2.8 us, 6.8 from call to call.
+// controlled, all filters: 6.9 us, with five wavefronts per SIMD (four, in 20 registers more: 7.6).  96 rows: 2.3 us, 6.8 from
+// call to call.
 template <bool FILTER>
-__global__ __launch_bounds__(256) void tabx_sample_actions_kernel(const ChoiceArgs a)
+__global__ __launch_bounds__(256, 5) void tabx_sample_actions_kernel(const ChoiceArgs a)
 {
     for (int64_t first = (int64_t)blockIdx.x * 256; first < a.rows; first += (int64_t)gridDim.x * 256) {
         const bool there = first + (int)threadIdx.x < a.rows;
@@ -285,10 +290,14 @@ __global__ __launch_bounds__(256) void tabx_sample_actions_kernel(const ChoiceAr
             const Weights8 w = weigh(s, a);
             float spare;
             choice = pick<FILTER>(s, w.w, a.how, uniform, spare);
-            for (uint64_t close = __ballot(on && some && spare <= 0.0f); close != 0; close &= close - 1) {
-                const int source = __builtin_ctzll(close);
+            uint64_t close = __ballot(on && some && spare <= 0.0f);
+            uint32_t left = (uint32_t)(close >> ((int)threadIdx.x & 56)) & 255;   // of this lane's eight rows
+            while (close != 0) {
+                const int source = ((int)threadIdx.x & 56) + (left != 0 ? __builtin_ctz(left) : 0);
                 const int exact = pick_exactly<FILTER>(s, a.how, uniform, a.inv_temperature64, source);
-                choice = ((int)threadIdx.x & 63) == source ? exact : choice;
+                choice = left != 0 && ((int)threadIdx.x & 63) == source ? exact : choice;
+                left &= left - 1;
+                close = __ballot(left != 0);
             }
             choice = some ? choice : TABX_ACT_NOOP;
             log_prob = some ? (score_of_choice(s, choice) - s.top) * a.inv_temperature - log_of_sum(w.others) : 0.0f;

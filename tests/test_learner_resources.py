@@ -36,3 +36,9 @@ def test_one_lane_per_row_needs_no_lds(listing):
     sizes = re.findall(r"\.amdhsa_kernel (_ZN4tabx\w+)\n\s+\.amdhsa_group_segment_fixed_size (\d+)", listing)
     rows = [(n, int(s)) for n, s in sizes if "sample_actions" in n or "log_prob" in n]
     assert len(rows) == 4 and all(s == 0 for _, s in rows), rows
+
+
+def test_draws_leave_room_for_five_wavefronts(listing):
+    """512 registers of a SIMD's lane, handed out in eights."""
+    sizes = re.findall(r"\.amdhsa_kernel (_ZN4tabx\w*sample_actions\w+)\n(?:.*\n)*?\s+\.amdhsa_next_free_vgpr (\d+)", listing)
+    assert len(sizes) == 2 and all(int(n) <= 96 for _, n in sizes), sizes
