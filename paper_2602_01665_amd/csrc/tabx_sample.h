@@ -395,7 +395,10 @@ __global__ __launch_bounds__(256) void tabx_log_prob_grad_kernel(const ChoiceArg
                 const float own = __builtin_amdgcn_exp2f(k.t), rest = k.t == 0.0f ? w.others : 1.0f + w.others - own;
                 const float mine = fmaf(gl * rest, by, own * fmaf(along, fmaxf(k.t, -200.0f), apart));
 #pragma unroll
-                for (int i = 0; i < kChoices; ++i) g[i] = k.action == i ? mine : w.w[i] * fmaf(along, w.t[i], both);
+                for (int i = 0; i < kChoices; ++i) {
+                    const float v = k.action == i ? mine : w.w[i] * fmaf(along, w.t[i], both);
+                    g[i] = s.l[i] > -INFINITY ? v : 0.0f;   // (zero times a gradient that is not finite would be none)
+                }
             }
         }
         if (a.stream) store_gradient<true>(g, a, r);
