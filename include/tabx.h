@@ -388,6 +388,9 @@ int tabx_row_form(const TabxParams *params, int call, TabxRowForm *form);
  * other calls; the device that owns `stream` and the arrays has to be the current one.  rows == 0
  * is a no-op that needs no arrays.  rows may not exceed 2^40, nor rows times a stride 2^60
  * (TABX_ERR_SHAPE).  Outputs must not overlap inputs or each other, except where it is said.
+ * As in the policy's calls, `controlled` marks the units that a call acts for.  Here these are the
+ * units that learn: next to a scripted side it is the complement of the array that the policy's
+ * calls take under that name.
  * ------------------------------------------------------------------------------------------- */
 
 /* Element types of the learner's arrays. */
@@ -405,15 +408,17 @@ typedef struct TabxRows {
 #define TABX_NORM_MAX_WIDTH 8192      /* widest row of the layer norm                      */
 #define TABX_SAMPLE_MAX_LEVELS 16384  /* most levels tabx_sample_levels chooses between    */
 
-/* Layer norm of every row with row_mask[r] != 0 (NULL: all; pass `controlled` to leave out the
- * units that do not learn):
+/* Layer norm of every row with row_mask[r] != 0 (NULL: all; where not all units learn, pass what the
+ * calls below take as `controlled`, the units that do):
  *   mean = sum_j x_j / width, rstd = 1 / sqrt(sum_j (x_j - mean)^2 / width + eps),
  *   y_j = (x_j - mean) * rstd * weight_j + bias_j,
  * in 32 bits, y rounded once to its type.  weight / bias: device [width] f32, NULL = all one / all
  * zero.  mean / rstd: device [rows] f32, both or neither; a backward pass needs them.
  * eps >= 0 and finite (TABX_ERR_PARAM); 1 <= width <= TABX_NORM_MAX_WIDTH (TABX_ERR_SHAPE).  Rows
- * that are masked out are neither read nor written, in any output.  y may be x itself (same data,
- * stride and type). */
+ * that are masked out are neither read nor written, in any output: where a later product takes all
+ * rows of y, let them hold finite values beforehand (with a gradient of zero, a row of zeros adds
+ * nothing to a weight's gradient; one of NaN makes it NaN).  y may be x itself (same data, stride
+ * and type). */
 int tabx_layer_norm(int64_t rows, int32_t width, const TabxRows *x, const uint8_t *row_mask,
                     const float *weight, const float *bias, float eps, const TabxRows *y,
                     float *mean, float *rstd, void *stream);
@@ -423,13 +428,13 @@ int tabx_layer_norm(int64_t rows, int32_t width, const TabxRows *x, const uint8_
  *   grad_x_j = rstd * (g_j - sum_j g_j / width - h_j * sum_j (g_j h_j) / width),
  *   grad_weight_j = sum over rows of grad_y_j h_j, grad_bias_j = sum over rows of grad_y_j.
  * Rows that are masked out are not read and add nothing; their grad_x is zero.  grad_x (NULL:
- * not wanted, as for an observation) may be grad_y itself (same data, stride and type).  grad_weight / grad_bias: device
- * [width] f32, overwritten (with zeros if there are no rows), each may be NULL.  The sums are always taken in the same order: equal
- * calls give equal bits.  `workspace`: device memory, 16-byte aligned, of at least
- * tabx_layer_norm_workspace(rows, width) bytes (TABX_ERR_SHAPE if workspace_bytes is less), needed
- * only for grad_weight and grad_bias.  Its contents need no preparation; it belongs to the call
- * until the enqueued work has finished, so calls (and replays of captured graphs) that may run at
- * the same time need one each. */
+ * not wanted, as for an observation) may be grad_y itself (same data, stride and type).
+ * grad_weight / grad_bias: device [width] f32, overwritten (with zeros if there are no rows), each
+ * may be NULL.  The sums are always taken in the same order: equal calls give equal bits.
+ * `workspace`: device memory, 16-byte aligned, of at least tabx_layer_norm_workspace(rows, width)
+ * bytes (TABX_ERR_SHAPE if workspace_bytes is less), needed only for grad_weight and grad_bias.  Its
+ * contents need no preparation; it belongs to the call until the enqueued work has finished, so calls
+ * (and replays of captured graphs) that may run at the same time need one each. */
 int tabx_layer_norm_backward(int64_t rows, int32_t width, const TabxRows *x,
                              const uint8_t *row_mask, const float *weight, const float *mean,
                              const float *rstd, const TabxRows *grad_y, const TabxRows *grad_x,

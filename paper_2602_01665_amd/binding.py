@@ -362,7 +362,8 @@ def _enqueue(what, function, device, stream, *args):
 
 
 def tabx_layer_norm(x, weight, bias, eps, y, mean=None, rstd=None, row_mask=None, stream=None):
-    """y = layer norm of the rows of x (over the last dimension) whose row_mask byte is not 0."""
+    """y = layer norm of the rows of x (over the last dimension) whose row_mask byte is not 0.  Other rows
+    of y keep what they hold: finite values, where a product will read them too."""
     what, f32, dev = "tabx_layer_norm", torch.float32, x.get_device()
     xr, rows = _rows(what, x, "x", 0)
     width = x.shape[-1]
@@ -649,13 +650,15 @@ class TabxEnv:
                           self.dones, self.obs, self.vis, self.amask, stream)
 
     def norm_obs(self, weight, bias, eps, y, mean=None, rstd=None, controlled=None, stream=None):
-        """y [E, N, D] = layer norm of the observation rows, of the controlled units (None: all)."""
+        """y [E, N, D] = layer norm of the observation rows, of the controlled units (None: all): those that
+        learn, not those that the policy's calls take as controlled.  Other rows of y keep what they hold."""
         tabx_layer_norm(self.obs, weight, bias, eps, y, mean, rstd, controlled, stream)
 
     def sample_actions(self, logits, sampling, uniform, actions, log_prob=None, controlled=None,
                        stream=None):
-        """Fills `actions` (uint8 [E, N], in place) for the controlled units (None: all) from their
-        logits [E, N, 8], where the last observation lets them strike."""
+        """Fills `actions` (uint8 [E, N], in place) for the controlled units (None: all; those that learn, not
+        those that the policy's calls take) from their logits [E, N, 8], with the combat action for those
+        that the last observation lets strike."""
         tabx_sample_actions(logits, sampling, uniform, actions, log_prob, self.amask, controlled,
                             stream)
         return actions
