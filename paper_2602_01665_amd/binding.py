@@ -268,9 +268,10 @@ def tabx_scripted_step_observe(params, scenario, state, policy, memory, controll
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
+# The calls are not part of PyTorch's graph: inputs count as detached, and each way back is a call of its own.
 # What a call on a few thousand rows costs is the time until it is enqueued: the checks are plain
-# functions of few steps (a small tabx_sample_actions takes the host 6.3 us, 10.1 as methods of an
-# object with torch.cuda.current_stream()).  `device` is that of a call's first tensor, -1 the host.
+# functions of few steps (a small tabx_sample_actions takes the host 6.4 us, 0.1 of them to tell PyTorch what
+# was written; 10.1 as methods of an object with torch.cuda.current_stream()).  `device` is that of a call's first tensor, -1 the host.
 
 
 def _refuse(what, why):
@@ -343,7 +344,9 @@ def _needed(what, t, name, count, dtype, device):
     return _array(what, t, name, count, dtype, device)
 
 
-def _enqueue(what, function, device, stream, *args):
+def _enqueue(what, function, device, stream, written, *args):
+    """Makes the call; `written`: the tensors it writes (or None), of which PyTorch's graph is told, so that a
+    backward pass that needs what they held before is refused, as after PyTorch's own calls in place."""
     if device < 0:
         _refuse(what, "the tensors are not on a GPU")
     if stream is None:
@@ -352,13 +355,14 @@ def _enqueue(what, function, device, stream, *args):
         raw = stream.cuda_stream
     else:
         _refuse(what, f"the stream is on {stream.device}, the tensors are on cuda:{device}")
-    if torch.cuda.current_device() == device:
+    if torch._C._cuda_getDevice() == device:
         rc = function(*args, raw)
     else:
         with torch.cuda.device(device):
             rc = function(*args, raw)
     if rc != 0:
         _check(rc, what)
+    torch._C._increment_version([t for t in written if t is not None])
 
 
 def tabx_layer_norm(x, weight, bias, eps, y, mean=None, rstd=None, row_mask=None, stream=None):
@@ -368,7 +372,7 @@ def tabx_layer_norm(x, weight, bias, eps, y, mean=None, rstd=None, row_mask=None
     xr, rows = _rows(what, x, "x", 0)
     width = x.shape[-1]
     yr = _same_rows(what, y, "y", width, dev, rows)
-    _enqueue(what, _lib.tabx_layer_norm, dev, stream, rows, width, C.byref(xr),
+    _enqueue(what, _lib.tabx_layer_norm, dev, stream, (y, mean, rstd), rows, width, C.byref(xr),
              _array(what, row_mask, "row_mask", rows, torch.uint8, dev),
              _array(what, weight, "weight", width, f32, dev),
              _array(what, bias, "bias", width, f32, dev), eps, C.byref(yr),
@@ -395,7 +399,8 @@ def tabx_layer_norm_backward(x, weight, mean, rstd, grad_y, grad_x=None, grad_we
     if grad_x is not None:
         ir = C.byref(_same_rows(what, grad_x, "grad_x", width, dev, rows))
     size = 0 if workspace is None else workspace.numel()
-    _enqueue(what, _lib.tabx_layer_norm_backward, dev, stream, rows, width, C.byref(xr),
+    _enqueue(what, _lib.tabx_layer_norm_backward, dev, stream, (grad_x, grad_weight, grad_bias), rows,
+             width, C.byref(xr),
              _array(what, row_mask, "row_mask", rows, torch.uint8, dev),
              _array(what, weight, "weight", width, f32, dev),
              _needed(what, mean, "mean", rows, f32, dev),
@@ -410,7 +415,7 @@ def tabx_sample_actions(logits, sampling, uniform, actions, log_prob=None, actio
     """Draws an action from each unit's eight logits, into `actions` (uint8, in place)."""
     what, f32, u8, dev = "tabx_sample_actions", torch.float32, torch.uint8, logits.get_device()
     lr, rows = _rows(what, logits, "logits", 8)
-    _enqueue(what, _lib.tabx_sample_actions, dev, stream, rows, C.byref(lr),
+    _enqueue(what, _lib.tabx_sample_actions, dev, stream, (actions, log_prob), rows, C.byref(lr),
              _array(what, action_mask, "action_mask", rows, u8, dev),
              _array(what, controlled, "controlled", rows, u8, dev), C.byref(sampling),
              _needed(what, uniform, "uniform", rows, f32, dev),
@@ -436,7 +441,7 @@ def tabx_sample_levels(scores, sampling, uniform, next_level, level_mask=None, e
     levels = scores.shape[-1]
     if n == 1:
         sr.stride = 0
-    _enqueue(what, _lib.tabx_sample_levels, dev, stream, envs, levels, C.byref(sr),
+    _enqueue(what, _lib.tabx_sample_levels, dev, stream, (next_level,), envs, levels, C.byref(sr),
              _array(what, level_mask, "level_mask", levels, u8, dev),
              _array(what, env_mask, "env_mask", envs, u8, dev), C.byref(sampling),
              _needed(what, uniform, "uniform", envs, torch.float32, dev),
@@ -448,7 +453,7 @@ def tabx_action_log_prob(logits, actions, temperature, log_prob, entropy=None, a
     """log_prob (and entropy) of the actions under the distribution of their logits."""
     what, f32, u8, dev = "tabx_action_log_prob", torch.float32, torch.uint8, logits.get_device()
     lr, rows = _rows(what, logits, "logits", 8)
-    _enqueue(what, _lib.tabx_action_log_prob, dev, stream, rows, C.byref(lr),
+    _enqueue(what, _lib.tabx_action_log_prob, dev, stream, (log_prob, entropy), rows, C.byref(lr),
              _array(what, action_mask, "action_mask", rows, u8, dev),
              _array(what, controlled, "controlled", rows, u8, dev),
              _needed(what, actions, "actions", rows, u8, dev), temperature,
@@ -463,7 +468,7 @@ def tabx_action_log_prob_backward(logits, actions, temperature, grad_log_prob, g
     dev = logits.get_device()
     lr, rows = _rows(what, logits, "logits", 8)
     gr = _same_rows(what, grad_logits, "grad_logits", 8, dev, rows)
-    _enqueue(what, _lib.tabx_action_log_prob_backward, dev, stream, rows, C.byref(lr),
+    _enqueue(what, _lib.tabx_action_log_prob_backward, dev, stream, (grad_logits,), rows, C.byref(lr),
              _array(what, action_mask, "action_mask", rows, u8, dev),
              _array(what, controlled, "controlled", rows, u8, dev),
              _needed(what, actions, "actions", rows, u8, dev), temperature,

@@ -44,3 +44,45 @@ def test_gradients_that_are_not_finite_stay_with_the_choices_allowed(B, dtype):
     assert bool((got[barred] == 0).all()) and bool((got[on == 0] == 0).all())
     assert torch.equal(got[~odd], want[~odd])
     assert bool(torch.isfinite(want).all())
+
+
+def test_a_graph_that_needs_what_was_overwritten_is_refused(B):
+    """The next tick's rows in the tensor that a network has kept for its backward pass, and the other
+    outputs the same: PyTorch refuses that pass, as after a call of its own in place."""
+    y, mean, rstd = torch.zeros(6, 16, device=DEV), torch.zeros(6, device=DEV), torch.zeros(6, device=DEV)
+    x, m = torch.randn(6, 16, device=DEV), torch.randn(16, 8, device=DEV, requires_grad=True)
+    B.tabx_layer_norm(x, None, None, 1e-5, y, mean, rstd)
+    out = (y @ m).sum()
+    out.backward(retain_graph=True)
+    B.tabx_layer_norm(x + 1, None, None, 1e-5, y)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        out.backward()
+    (y @ m).sum().backward()
+
+
+def test_what_each_call_writes_is_told(B):
+    f = lambda *s: torch.rand(*s, device=DEV)  # noqa: E731
+    e = 40
+    x, gy, z, w = f(e, 16), f(e, 16), f(e, 8), f(16)
+    acts, nxt = torch.zeros(e, dtype=torch.uint8, device=DEV), torch.zeros(e, dtype=torch.int32, device=DEV)
+    o = {k: f(e) for k in ("mean", "rstd", "u", "lp", "h")}
+    o.update(y=f(e, 16), gx=f(e, 16), gw=f(16), gb=f(16), gz=f(e, 8), x=x, gy=gy, z=z, w=w, acts=acts, nxt=nxt)
+    ws = torch.empty(B.tabx_layer_norm_workspace(e, 16), dtype=torch.uint8, device=DEV)
+    how = B.TabxSampling()
+
+    def writes(names, call, *args):
+        before = {k: t._version for k, t in o.items()}
+        call(*args)
+        assert {k for k, t in o.items() if t._version != before[k]} == set(names.split()), names
+
+    writes("y", B.tabx_layer_norm, x, w, None, 1e-5, o["y"])
+    writes("y mean rstd", B.tabx_layer_norm, x, w, None, 1e-5, o["y"], o["mean"], o["rstd"])
+    writes("gx", B.tabx_layer_norm_backward, x, w, o["mean"], o["rstd"], gy, o["gx"])
+    writes("gw gb", B.tabx_layer_norm_backward, x, w, o["mean"], o["rstd"], gy, None, o["gw"], o["gb"], ws)
+    writes("acts", B.tabx_sample_actions, z, how, o["u"], acts)
+    writes("acts lp", B.tabx_sample_actions, z, how, o["u"], acts, o["lp"])
+    writes("nxt", B.tabx_sample_levels, w, how, o["u"], nxt)
+    writes("lp h", B.tabx_action_log_prob, z, acts, 1.0, o["lp"], o["h"])
+    writes("gz", B.tabx_action_log_prob_backward, z, acts, 1.0, o["lp"], None, o["gz"])
+    with torch.inference_mode():               # (whose tensors have no versions)
+        B.tabx_layer_norm(x, w, None, 1e-5, f(e, 16))
