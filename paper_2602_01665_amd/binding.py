@@ -664,12 +664,20 @@ class TabxEnv:
         """Fills `actions` (uint8 [E, N], in place) for the controlled units (None: all; those that learn, not
         those that the policy's calls take) from their logits [E, N, 8], with the combat action for those
         that the last observation lets strike."""
+        if self.amask is None:
+            _refuse("sample_actions", "this batch keeps no action mask (want_action_mask=False)")
         tabx_sample_actions(logits, sampling, uniform, actions, log_prob, self.amask, controlled,
                             stream)
         return actions
 
     def sample_levels(self, scores, sampling, uniform, level_mask=None, env_mask=None, stream=None):
-        """Draws the levels that the envs' next episodes take (instead of the uniform draw)."""
+        """Draws the levels that the envs' next episodes take (instead of the uniform draw), out of the
+        batch's num_levels."""
+        levels = self.p.get("num_levels", 0)
+        if levels < 1:
+            _refuse("sample_levels", "this batch has no bank of levels (num_levels)")
+        if scores.dim() and scores.shape[-1] != levels:    # (a reset takes next_level modulo num_levels)
+            _refuse("sample_levels", f"scores has rows of {scores.shape[-1]} elements, not {levels}")
         tabx_sample_levels(scores, sampling, uniform, self.st["next_level"], level_mask, env_mask,
                            stream)
 

@@ -182,3 +182,34 @@ def test_tensors_are_checked_before_their_addresses_are_taken(B):
     refused("not on a GPU", B.tabx_action_log_prob_backward, lg, acts, 1.0, u, u, lg)
     refused("grad_logits has 5", B.tabx_action_log_prob_backward, lg, acts, 1.0, u, u, lg[:5])
     assert f is x.dtype
+
+
+def test_a_batch_refuses_draws_that_would_mean_something_else(B):
+    """Actions without the observation's mask; levels without a bank, or out of another number of them."""
+    from paper_2602_01665_amd import inputs as I
+    w = I.WORKLOADS["c2_4096env_5v5"]
+
+    def env(E, **kw):
+        over = {k: kw.pop(k) for k in ("num_levels",) if k in kw}
+        return B.TabxEnv(I.make_params(w, E, **over), I.make_scenario(w, over.get("num_levels", E)), device="cpu", **kw)
+
+    how, u = B.TabxSampling(), torch.zeros(4)
+    one = env(4, want_action_mask=False)
+    acts = torch.zeros(4, one.N, dtype=torch.uint8)
+    logits = torch.zeros(4, one.N, 8)
+    for batch in [one] + one.parts(1):
+        with pytest.raises(B.TabxError, match="no action mask"):
+            batch.sample_actions(logits, how, torch.zeros(4, one.N), acts)
+        with pytest.raises(B.TabxError, match="no bank of levels"):
+            batch.sample_levels(torch.zeros(3), how, u)
+    bank = env(4, num_levels=6)
+    for batch in [bank] + bank.parts(1):
+        for wrong in (torch.zeros(5), torch.zeros(7), torch.zeros(4, 12)):
+            with pytest.raises(B.TabxError, match="not 6"):
+                batch.sample_levels(wrong, how, u)
+        with pytest.raises(B.TabxError, match="no dimensions"):
+            batch.sample_levels(torch.zeros(()), how, u)
+        with pytest.raises(B.TabxError, match="not on a GPU"):      # what is left to refuse on the host
+            batch.sample_levels(torch.zeros(6), how, u)
+        with pytest.raises(B.TabxError, match="not on a GPU"):
+            batch.sample_actions(logits, how, torch.zeros(4, one.N), acts)
