@@ -72,7 +72,7 @@ constexpr int64_t kComputeUnits = 256;
 constexpr int64_t kL2Bytes = 32 << 20;             // eight L2s of 4 MB
 constexpr int64_t kSideCacheBytes = 256 << 20;     // the cache on the memory's side
 constexpr int64_t kMostGroups = (int64_t)1 << 20;  // of a launch; beyond them its teams or lanes take several turns
-constexpr int64_t kNormTeams = 81920;              // teams that share the rows of a forward call, if they are many
+constexpr int64_t kNormTeams = 10 * 8192;          // teams that share the rows of a forward call, if they are many
 constexpr int64_t kGradTurns = 4;                  // turns of a team's run of rows in a backward call
 constexpr int64_t kAloneGroups = 2;                // workgroups whose rows one takes alone in a backward call
 
@@ -104,11 +104,19 @@ static int for_width(int pieces, const Args &...args)
     return TABX_ERR_SHAPE;
 }
 
-// A team takes its rows in one turn or two and is done, but for the widest rows: there every workgroup would load as much
-// of weight and bias as it has rows, so the machine's lanes stay (rows of 4096: 74 us, 63; of 6000: 139, 102; rows of 2144
-// are faster without, 250 and 261).
-// What is written and is more than the L2s hold goes past them (22 MB on from where they are full: 28.6 us, 23.1; 10v10 x
-// 16384: 76 us, 71), but in pieces of a third of a line it does not (rows of 184 elements: 85 us, 87; of 186: 87.6, 91.5).
+// Ten times as many teams as the machine holds wavefronts: short runs go through memory in its order, but a team of one turn
+// has no next rows under way.  10240, 20480, 40960, 81920, 163840, 655360 of them: 200000 rows of 700 bf16 131, 125, 118, 114,
+// 115, 135 us; a million of 128 bf16 99, 102, 96, 86, 90, 115; 655360 of 160 f32 130, 126, 117, 116, 129, 129; 700000 of 96 f32,
+// half of them, 47, 44, 42, 44, 47, 60.
+// The widest rows' teams stay: every workgroup would load as much of weight and bias as it has rows (rows of 4096: 74 us, 63; of
+// 6000: 139, 102; rows of 2144 are faster without, 250 and 261).
+// What is written and is more than the L2s hold goes past them (60000 rows of 368 to bf16: 29.0 us, 22.7; 150000: 68.1, 66.4;
+// f32 of any width 2 to 7 % less), but not where each store of a row is a line's length and lies across two of them: sixteen
+// lanes' pieces of 16-bit results, in rows off the half lines (90 MB from bf16, past the caches or not: 66 98.8, 93.0 us, 130
+// 96.1, 88.4, 186 83.1, 78.5; on them 128 64.8, 68.2, 160 74.4, 76.1, 192 65.2, 68.1).  Rows of a single piece gain and lose
+// as much (56: 73.3, 78.3; 50: 85.8, 82.5), those of more lanes lose next to nothing (196 to 2050 elements: -8 to 1 %; 254: 4 %).
+// Rows that are masked out count, as the host does not see them; a call that writes half of that gains too (22 MB of 44: 16.2
+// us, 13.8).
 template <int LANES, int PIECES>
 struct NormForward {
     static constexpr bool kUsed = true;
@@ -119,7 +127,8 @@ struct NormForward {
         a.team_rows = LANES <= 64 ? least(quotient_up(quotient_up(a.rows, kNormTeams), at_once(LANES)) * at_once(LANES), 64) : 1;
         const int64_t groups = least(quotient_up(a.rows, a.team_rows * teams), stays ? kComputeUnits * 2048 / LANES : kMostGroups);
         a.lap = groups * teams * a.team_rows;
-        a.stream = !(LANES == 16 && PIECES == 3) && a.rows * a.width * size_of(a.y_type) > kL2Bytes;
+        const bool across = LANES == 16 && PIECES > 1 && a.y_type != TABX_F32 && !(on_boundary(a.y, 64) && a.y_stride % 32 == 0);
+        a.stream = !across && a.rows * a.width * size_of(a.y_type) > kL2Bytes;
         return a.x_type == TABX_F32 ? launch(tabx_norm_kernel<LANES, PIECES, 4>, groups, threads_of(LANES), a, stream)
                                     : launch(tabx_norm_kernel<LANES, PIECES, 2>, groups, threads_of(LANES), a, stream);
     }

@@ -359,8 +359,9 @@ __global__ __launch_bounds__(threads_of(LANES)) void tabx_norm_kernel(const Norm
 // through the rows in the order of their addresses all the same (200000 rows of 512 in bf16 136 us with a long run per
 // team, 121 with runs of four rows, 5.1 TB/s; 85051 rows 61 and 56).
 // ONCE: more is read than the memory-side cache holds, so nothing of it is kept (10v10 x 16384 without the input's
-// gradient, 364 MB: 64 us, 5.7 TB/s, 70 without; 90 MB: 20.8 and 20.4; with the input's gradient it is slower, 182 us
-// and 171, 200000 rows of 700).
+// gradient, 364 MB: 64 us, 5.7 TB/s, 69 without; 66 MB: 14.4 and 13.3; with the input's gradient it is slower, 182 us
+// and 171, 200000 rows of 700).  Rows that are masked out count, as the host does not see them; a call that reads half of
+// that gains too (132 MB of 265: 28.6 us and 31.3).
 template <int LANES, int PIECES, int X_BYTES, int G_BYTES, bool INPUTS, bool ONCE>
 __global__ __launch_bounds__(threads_of(LANES), grad_wavefronts(PIECES)) void tabx_norm_grad_kernel(const NormArgs a)
 {

@@ -86,3 +86,20 @@ def test_what_each_call_writes_is_told(B):
     writes("gz", B.tabx_action_log_prob_backward, z, acts, 1.0, o["lp"], None, o["gz"])
     with torch.inference_mode():               # (whose tensors have no versions)
         B.tabx_layer_norm(x, w, None, 1e-5, f(e, 16))
+
+
+@pytest.mark.parametrize("rows,width,pad,tx,ty,offset", [
+    (100000, 186, 0, torch.float32, torch.float32, 0), (120000, 160, 0, torch.bfloat16, torch.bfloat16, 0),
+    (140001, 128, 0, torch.bfloat16, torch.float16, 1), (140001, 128, 32, torch.float32, torch.bfloat16, 32),
+    (130001, 130, 0, torch.bfloat16, torch.bfloat16, 0), (300001, 56, 0, torch.float16, torch.bfloat16, 0)])
+def test_results_past_the_caches_are_those_of_few_rows(B, rows, width, pad, tx, ty, offset):
+    """Rows on and off the boundaries of lines, of one piece and of more."""
+    print("[gpu] norm", rows, width, pad, tx, ty, offset, flush=True)
+    g = torch.Generator(device=DEV).manual_seed(rows)
+    x, w = torch.randn(rows, width, generator=g, device=DEV).to(tx), torch.randn(width, generator=g, device=DEV)
+    out = [torch.full((offset + rows * (width + pad),), 3.0, dtype=ty, device=DEV) for _ in range(2)]
+    whole, parts = (t[offset:].view(rows, width + pad)[:, :width] for t in out)
+    B.tabx_layer_norm(x, w, None, 1e-5, whole)
+    for a in range(0, rows, 9000):
+        B.tabx_layer_norm(x[a:a + 9000], w, None, 1e-5, parts[a:a + 9000])
+    assert torch.equal(*out)
