@@ -91,7 +91,8 @@ class TabxSampling(C.Structure):
                 ("min_p", C.c_float)]
 
     def __init__(self, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
-        super().__init__(temperature, top_k, top_p, min_p)
+        # more choices than there can be are all; what 32 bits do not hold would be cut off
+        super().__init__(temperature, max(-1, min(top_k, 2 ** 31 - 1)), top_p, min_p)
 
 
 def load_library(path: str = LIB_PATH) -> C.CDLL:
@@ -266,6 +267,7 @@ def tabx_scripted_step_observe(params, scenario, state, policy, memory, controll
 # --- the learner's side of the tick: tensors of its own, checked before their addresses are taken ---
 
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_MOST = 2 ** 31 - 1                     # (ctypes would cut off what a 32-bit argument does not hold)
 
 
 # The calls are not part of PyTorch's graph: inputs count as detached, and each way back is a call of its own.
@@ -294,6 +296,8 @@ def _rows(what, t, name, width, device=None):
     wide = shape[-1]
     if wide != width and width:
         _refuse(what, f"{name} has rows of {wide} elements, not {width}")
+    if wide > _MOST:
+        _refuse(what, f"{name} has rows of {wide} elements")
     if device is not None and t.get_device() != device:
         _elsewhere(what, t, name, device)
     if t.is_contiguous():
@@ -382,6 +386,8 @@ def tabx_layer_norm(x, weight, bias, eps, y, mean=None, rstd=None, row_mask=None
 
 def tabx_layer_norm_workspace(rows: int, width: int) -> int:
     """Bytes of workspace that tabx_layer_norm_backward needs for the weight's and bias's gradients."""
+    if not (-1 <= width <= _MOST and -1 <= rows < 2 ** 63):
+        _refuse("tabx_layer_norm_workspace", f"{rows} rows of {width} elements")
     n = _lib.tabx_layer_norm_workspace(rows, width)
     if n < 0:
         _check(n, "tabx_layer_norm_workspace")

@@ -213,3 +213,26 @@ def test_a_batch_refuses_draws_that_would_mean_something_else(B):
             batch.sample_levels(torch.zeros(6), how, u)
         with pytest.raises(B.TabxError, match="not on a GPU"):
             batch.sample_actions(logits, how, torch.zeros(4, one.N), acts)
+
+
+def test_sizes_that_32_bits_do_not_hold_are_not_cut_off(B):
+    wide = torch.empty(2, 2 ** 32 + 8, device="meta")
+    x, how, u8 = torch.zeros(2, 8), B.TabxSampling(), torch.zeros(2, dtype=torch.uint8)
+
+    def refused(call, *args):
+        with pytest.raises(B.TabxError, match="rows of 4294967304"):
+            call(*args)
+
+    refused(B.tabx_layer_norm, wide, None, None, 1e-5, wide)
+    refused(B.tabx_layer_norm, x, None, None, 1e-5, wide)
+    refused(B.tabx_layer_norm_backward, wide, None, x[:, 0], x[:, 0], wide, wide)
+    refused(B.tabx_layer_norm_workspace, 2, 2 ** 32 + 8)
+    refused(B.tabx_sample_levels, wide, how, x[:, 0], torch.zeros(2, dtype=torch.int32))
+    refused(B.tabx_sample_levels, wide[0], how, x[:, 0], torch.zeros(2, dtype=torch.int32))
+    refused(B.tabx_sample_actions, wide, how, x[:, 0], u8)
+    assert B.TabxSampling(1.0, 2 ** 32 + 5).top_k == 2 ** 31 - 1 and B.TabxSampling(1.0, 5).top_k == 5
+    assert B.TabxSampling(1.0, -2 ** 32 + 5).top_k < 0            # refused by every call
+    assert B.tabx_layer_norm_workspace(2 ** 40, 8) > 0
+    for rows in (2 ** 64 + 4, 2 ** 63, -2 ** 64 + 4):
+        with pytest.raises(B.TabxError):
+            B.tabx_layer_norm_workspace(rows, 8)
