@@ -309,9 +309,11 @@ __device__ __forceinline__ uint64_t threshold(uint32_t (&key)[ITEMS], const uint
 }
 
 // THREADS threads hold ITEMS levels each.  EACH: the running sums of single levels fit into LDS; else those of four.
-// Bound by its own latency: two trips to memory, the weights, and a dozen barriers for each threshold.  16384 envs, one
-// table of 4096: 6.3 us (3.7 at temperature 0, which needs no weights), top_k 8.6, top_p 8.3, both 10.4; 5003 envs, 257
-// levels: 4.1.  4096 envs with tables of 2048 of their own: 24 us, with both 41.
+// One table of up to 4096 levels is bound by its own latency: two trips to memory, the weights, and a dozen barriers for each
+// threshold.  16384 envs, 4096 levels: 6.3 us (3.7 at temperature 0, which needs no weights), top_k 8.6, top_p 8.3, both 10.4,
+// of which the vector instructions take 4.5; 5003 envs, 257 levels: 4.1.  More levels, or tables of the envs' own, are bound by
+// vector instructions, most of them for the weights and for numbers of 64 bits: 4096 envs with tables of 2048 22 us (14.5 of
+// instructions), with both 38 (23.9); one table of 16384 with both 28 (17.4).
 template <int THREADS, int ITEMS, bool EACH>
 __global__ __launch_bounds__(THREADS) void tabx_sample_levels_kernel(const LevelArgs a)
 {
