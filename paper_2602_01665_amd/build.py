@@ -12,8 +12,8 @@ LEARNER_SOURCES = [os.path.join(_PKG, "csrc", "tabx_learner.hip")]      # the le
 HEADERS = [os.path.join(_ROOT, "include", "tabx.h")] + [
     os.path.join(_PKG, "csrc", h)
     for h in ("tabx_device.h", "tabx_policy.h", "tabx_step.h", "tabx_observe.h",
-              "tabx_observe_packed.h", "tabx_rows.h", "tabx_norm.h", "tabx_sample.h",
-              "tabx_levels.h")]
+              "tabx_observe_packed.h", "tabx_rows.h", "tabx_teams.h", "tabx_host.h", "tabx_norm.h",
+              "tabx_sample.h", "tabx_levels.h")]
 LIB_PATH = os.path.join(_PKG, "libtabx.so")
 
 HIPCC_FLAGS = [
