@@ -393,8 +393,9 @@ int tabx_row_form(const TabxParams *params, int call, TabxRowForm *form);
  * calls take under that name.
  * ------------------------------------------------------------------------------------------- */
 
-/* Element types of the learner's arrays. */
-enum TabxType { TABX_F32 = 0, TABX_BF16 = 1, TABX_F16 = 2 };
+/* Element types of the learner's arrays.  The last two only where it is said: eight bits with four of
+ * exponent and three of fraction, finite up to 448, one NaN (OCP E4M3); and whole numbers. */
+enum TabxType { TABX_F32 = 0, TABX_BF16 = 1, TABX_F16 = 2, TABX_E4M3 = 3, TABX_I32 = 4 };
 
 /* Rows of a two-dimensional device array: element j of row r is data[r * stride + j], so the rows
  * may be some columns of a wider array.  `data` is aligned to its element only (TABX_ERR_ALIGN).
@@ -511,6 +512,148 @@ int tabx_action_log_prob_backward(int64_t rows, const TabxRows *logits, const ui
                                   double temperature, const float *grad_log_prob,
                                   const float *grad_entropy, const TabxRows *grad_logits,
                                   void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * A unit's memory.  A unit sees a part of the map; what it has seen before its network has to keep,
+ * over the ticks of an episode and no longer.  These calls are what such a network does on the
+ * batch's own arrays: the norm of its residual stream, queries and keys turned by the episode's tick
+ * (TabxState.t) and the unit's place (TabxState.x / y), and a memory that fades from tick to tick
+ * (linear attention with a decay for each head) and is forgotten where `dones` says that an episode
+ * has ended: one tick of a rollout, or the many ticks of an update with their gradients.  Rules of
+ * streams, errors and `rows` are those of the learner's calls.
+ * ------------------------------------------------------------------------------------------- */
+
+/* Root-mean-square norm of every row with row_mask[r] != 0 (NULL: all), behind a residual addition:
+ *   s_j = x_j + residual_j (x_j where residual is NULL), in 32 bits, rounded to the type of `sum` and
+ *     written there if that is given,
+ *   rstd = 1 / sqrt(sum_j s_j^2 / width + eps), y_j = s_j * rstd * weight_j,
+ * in 32 bits, y rounded once to its type.  weight: device [width] f32, NULL = all one.  rstd: device
+ * [rows] f32 (NULL: not wanted); a backward pass needs it, and `sum` (or x, if nothing was added).
+ * y may be of type TABX_E4M3, with a scale for each row: scale[r] = max(max_j |y_j| / 448, 2^-126) and y
+ * holds y_j / scale[r], rounded (scale: device [rows] f32, NULL iff y is of another type).  An element
+ * that is not a number is left out of the largest and stays one.
+ * eps >= 0 and finite (TABX_ERR_PARAM); 1 <= width <= TABX_NORM_MAX_WIDTH (TABX_ERR_SHAPE).  Rows that
+ * are masked out are neither read nor written, in any output.  `sum` may be x or residual itself, or
+ * y may, if `sum` is not the same (same data, stride and type). */
+int tabx_rms_norm(int64_t rows, int32_t width, const TabxRows *x, const TabxRows *residual,
+                  const uint8_t *row_mask, const float *weight, float eps, const TabxRows *sum,
+                  const TabxRows *y, float *scale, float *rstd, void *stream);
+
+/* Its gradients, from the sum and rstd of the forward call, the gradient of y (taken as not rounded)
+ * and that of `sum`, which comes along the residual stream (grad_sum NULL: none):
+ *   h_j = s_j * rstd, g_j = grad_y_j * weight_j,
+ *   grad_x_j = rstd * (g_j - h_j * sum_j (g_j h_j) / width) + grad_sum_j, x's gradient and the residual's,
+ *   grad_weight_j = sum over rows of grad_y_j h_j.
+ * grad_sum is of the type of `sum` (TABX_ERR_SHAPE).  grad_x (NULL: not wanted) may be grad_y or grad_sum
+ * itself (same data, stride and type); it is zero for rows that are masked out, of which nothing is
+ * read.  grad_weight: device [width] f32 (NULL: not wanted), overwritten; sums are always taken in the
+ * same order.  `workspace`: as in tabx_layer_norm_backward, tabx_rms_norm_workspace(rows, width) bytes,
+ * needed only for grad_weight. */
+int tabx_rms_norm_backward(int64_t rows, int32_t width, const TabxRows *sum, const uint8_t *row_mask,
+                           const float *weight, const float *rstd, const TabxRows *grad_y,
+                           const TabxRows *grad_sum, const TabxRows *grad_x, float *grad_weight,
+                           void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace of a tabx_rms_norm_backward call; host only.  Negative TabxError. */
+int64_t tabx_rms_norm_workspace(int64_t rows, int32_t width);
+
+/* Heads of rows, over ticks: element d of head h of row r at tick t is
+ *   data[t * tick_stride + r * row_stride + h * head_stride + d],
+ * so queries, keys and values may be columns of one array, and ticks may come before rows or behind
+ * them.  `data` is aligned to its element only (TABX_ERR_ALIGN).  Strides are not negative, and no
+ * element lies 2^60 or more behind the first (TABX_ERR_SHAPE); those of an input may be 0 (the same
+ * head for all); in an output no two elements share their place (each stride passes over what the
+ * smaller ones span: TABX_ERR_SHAPE). */
+typedef struct TabxHeads {
+    void    *data;
+    int64_t  tick_stride, row_stride, head_stride;     /* in elements                         */
+    int32_t  type;                                     /* TABX_F32, TABX_BF16 or TABX_F16      */
+} TabxHeads;
+
+#define TABX_ROTARY_MAX_WIDTH 512     /* widest head of tabx_rotary                            */
+#define TABX_ROTARY_MAX_AXES 4
+#define TABX_ATTENTION_MAX_WIDTH 128  /* widest key and value of the linear attention          */
+#define TABX_ATTENTION_MAX_HEADS 65536
+
+/* One axis of the rotation: where along it a row is, position[r / units] (units >= 1, a divisor of rows;
+ * TABX_ERR_SHAPE: 1 for a position of each unit, the batch's N for one of each env), of type TABX_I32
+ * or TABX_F32, and how many pairs turn with it (>= 0). */
+typedef struct TabxAxis {
+    const void *position;
+    int32_t     type, units, pairs;
+} TabxAxis;
+
+/* Turns pairs of every head's elements: the first axis' pairs come first, then the next one's.  Pair
+ * i of all P is (x_i, x_{P + i}), or (x_{2 i}, x_{2 i + 1}) if `interleaved` is not 0; by the angle
+ * a_i = position * frequency_i (in 64 bits; negative if `inverse` is not 0):
+ *   (u, v) -> (u cos a - v sin a, u sin a + v cos a), in 32 bits, rounded once to y's type.
+ * Elements from 2 P on are copied.  The gradient of x is the same call with `inverse` on the gradient
+ * of y.  frequency: device [P] f64, radians per unit of position.  row_mask: as in tabx_rms_norm.  A position
+ * that is not finite gives NaN.  x and y have the same type (TABX_ERR_SHAPE); y may be x itself (same data and
+ * strides).  1 <= num_axes <= TABX_ROTARY_MAX_AXES, heads >= 1, 2 <= width <= TABX_ROTARY_MAX_WIDTH,
+ * 2 <= 2 P <= width (TABX_ERR_SHAPE).  tick_stride is not looked at. */
+int tabx_rotary(int64_t rows, int32_t heads, int32_t width, const TabxHeads *x,
+                const uint8_t *row_mask, const TabxAxis *axes, int32_t num_axes,
+                const double *frequency, int32_t interleaved, int32_t inverse, const TabxHeads *y,
+                void *stream);
+
+/* A unit's memory: head h of row r holds a state S [key_width][value_width], and at every tick t
+ *   S <- e_h S (0 where the tick is the first of an episode), S <- S + k_t v_t^T,
+ *   out_t = scale * q_t S,
+ * with e_h = exp(log_decay[h]) (device [heads] f32; a value above 0, or NaN, is taken as 0; -infinity keeps
+ * nothing), in 32 bits, out rounded once to its type.
+ *   q, k [tick][row][head][key_width], v, out [tick][row][head][value_width]: one type for all of them,
+ *     f32, bf16 or f16 (TABX_ERR_SHAPE);
+ *   fresh [tick][rows / units] u8, units >= 1 a divisor of rows (TABX_ERR_SHAPE): not 0 where a row's tick is
+ *     the first of an episode, that is where `dones` was set by the tick before (NULL: nowhere);
+ *   controlled [rows] u8: rows of 0 are neither read nor written (NULL: all are);
+ *   states are [rows][heads][key_width][value_width] f32, without gaps.
+ * scale is finite (TABX_ERR_PARAM).  1 <= heads <= TABX_ATTENTION_MAX_HEADS, rows * heads <= 2^31 - 1, ticks <= 2^30,
+ * 1 <= key_width, value_width <= TABX_ATTENTION_MAX_WIDTH (TABX_ERR_SHAPE).  No rows: nothing to do.
+ * A value that is not finite reaches its own head from its tick on, until an episode ends.
+ *
+ * tabx_linear_attention_step: one tick of a rollout (strides of ticks are not looked at; fresh [rows / units],
+ * normally `dones` as the tick call before it left them).  `state` is updated where it lies. */
+int tabx_linear_attention_step(int64_t rows, int32_t heads, int32_t key_width, int32_t value_width,
+                               const TabxHeads *q, const TabxHeads *k, const TabxHeads *v,
+                               const float *log_decay, float scale, const uint8_t *fresh,
+                               int32_t units, const uint8_t *controlled, float *state,
+                               const TabxHeads *out, void *stream);
+
+/* Many ticks at once, from state_in (NULL: zero; not written) to state_out (NULL: not wanted; may be
+ * state_in).  No ticks: state_out is state_in, or zero.  The same sums as the steps' in another order.
+ * `workspace`: device memory, 16-byte aligned, of at least tabx_linear_attention_workspace() bytes
+ * (TABX_ERR_SHAPE if workspace_bytes is less; may be NULL if that is 0), whose contents need no
+ * preparation; calls (and replays of captured graphs) that may run at the same time need one each. */
+int tabx_linear_attention(int64_t ticks, int64_t rows, int32_t heads, int32_t key_width,
+                          int32_t value_width, const TabxHeads *q, const TabxHeads *k,
+                          const TabxHeads *v, const float *log_decay, float scale,
+                          const uint8_t *fresh, int32_t units, const uint8_t *controlled,
+                          const float *state_in, float *state_out, const TabxHeads *out,
+                          void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace of such a call, forward or backward; host only.  Negative TabxError. */
+int64_t tabx_linear_attention_workspace(int64_t ticks, int64_t rows, int32_t heads,
+                                        int32_t key_width, int32_t value_width);
+
+/* The gradients of q, k, v and state_in (each may be NULL: not wanted, but not all), from those of out
+ * and of state_out (grad_state_out NULL: zero), with S_t as above and
+ *   D_t = scale * q_t grad_out_t^T + e_h D_{t+1} (without the last part where tick t + 1 is the first of
+ *     an episode; after the last tick e_h D is grad_state_out),
+ *   grad_q_t = scale * S_t grad_out_t, grad_k_t = D_t v_t, grad_v_t = D_t^T k_t,
+ *   grad_state_in = e_h D_0 (0 where tick 0 is the first of an episode).
+ * log_decay is a setting and has no gradient.  All of the arrays are of one type.  Rows that are not
+ * controlled have gradients of zero, and nothing of them is read.  grad_state_in may be grad_state_out.
+ * A value that is not finite may reach the gradients of other ticks of its row and head, in any episode. */
+int tabx_linear_attention_backward(int64_t ticks, int64_t rows, int32_t heads, int32_t key_width,
+                                   int32_t value_width, const TabxHeads *q, const TabxHeads *k,
+                                   const TabxHeads *v, const float *log_decay, float scale,
+                                   const uint8_t *fresh, int32_t units, const uint8_t *controlled,
+                                   const float *state_in, const float *grad_state_out,
+                                   const TabxHeads *grad_out, const TabxHeads *grad_q,
+                                   const TabxHeads *grad_k, const TabxHeads *grad_v,
+                                   float *grad_state_in, void *workspace, int64_t workspace_bytes,
+                                   void *stream);
 
 const char *tabx_strerror(int code);
 

@@ -28,7 +28,10 @@ EXPORTS = ("tabx_obs_dim", "tabx_num_actions", "tabx_reset", "tabx_step", "tabx_
            "tabx_policy_step_observe", "tabx_scripted_step_observe", "tabx_part", "tabx_launch_info",
            "tabx_row_form", "tabx_layer_norm", "tabx_layer_norm_backward",
            "tabx_layer_norm_workspace", "tabx_sample_actions", "tabx_sample_levels",
-           "tabx_action_log_prob", "tabx_action_log_prob_backward", "tabx_strerror")
+           "tabx_action_log_prob", "tabx_action_log_prob_backward", "tabx_rms_norm",
+           "tabx_rms_norm_backward", "tabx_rms_norm_workspace", "tabx_rotary",
+           "tabx_linear_attention_step", "tabx_linear_attention", "tabx_linear_attention_backward",
+           "tabx_linear_attention_workspace", "tabx_strerror")
 
 _I8 = C.POINTER(C.c_int8)
 _I32 = C.POINTER(C.c_int32)
@@ -84,6 +87,16 @@ class TabxRows(C.Structure):
     _fields_ = [("data", C.c_void_p), ("stride", C.c_int64), ("type", C.c_int32)]
 
 
+class TabxHeads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("tick_stride", C.c_int64), ("row_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("type", C.c_int32)]
+
+
+class TabxAxis(C.Structure):
+    _fields_ = [("position", C.c_void_p), ("type", C.c_int32), ("units", C.c_int32),
+                ("pairs", C.c_int32)]
+
+
 class TabxSampling(C.Structure):
     """How a choice is drawn: temperature (0: the largest score), top_k (0: all), top_p (1: all),
     min_p (0: all)."""
@@ -125,9 +138,21 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.tabx_sample_levels.argtypes = [I64, I32, R, V, V, W, V, V, V]
     lib.tabx_action_log_prob.argtypes = [I64, R, V, V, V, F64, V, V, V]
     lib.tabx_action_log_prob_backward.argtypes = [I64, R, V, V, V, F64, V, V, R, V]
+    lib.tabx_rms_norm.argtypes = [I64, I32, R, R, V, V, F32, R, R, V, V, V]
+    lib.tabx_rms_norm_backward.argtypes = [I64, I32, R, V, V, V, R, R, R, V, V, I64, V]
+    lib.tabx_rms_norm_workspace.argtypes = [I64, I32]
+    H = C.POINTER(TabxHeads)
+    lib.tabx_rotary.argtypes = [I64, I32, I32, H, V, C.POINTER(TabxAxis), I32, V, I32, I32, H, V]
+    lib.tabx_linear_attention_step.argtypes = [I64, I32, I32, I32, H, H, H, V, F32, V, I32, V, V, H, V]
+    lib.tabx_linear_attention.argtypes = [I64, I64, I32, I32, I32, H, H, H, V, F32, V, I32, V, V, V, H,
+                                          V, I64, V]
+    lib.tabx_linear_attention_backward.argtypes = [I64, I64, I32, I32, I32, H, H, H, V, F32, V, I32, V, V,
+                                                   V, H, H, H, H, V, V, I64, V]
+    lib.tabx_linear_attention_workspace.argtypes = [I64, I64, I32, I32, I32]
     for name in EXPORTS[:-1]:
         getattr(lib, name).restype = C.c_int
-    lib.tabx_layer_norm_workspace.restype = I64
+    for name in ("tabx_layer_norm_workspace", "tabx_rms_norm_workspace", "tabx_linear_attention_workspace"):
+        getattr(lib, name).restype = I64
     return lib
 
 
@@ -285,11 +310,11 @@ def _elsewhere(what, t, name, device):
     _refuse(what, f"{name} is on {t.device}, not on {place}")
 
 
-def _rows(what, t, name, width, device=None):
+def _rows(what, t, name, width, device=None, types=TYPES):
     """(TabxRows, rows) of a tensor [..., width] whose rows lie at equal distances."""
-    code = TYPES.get(t.dtype)
+    code = types.get(t.dtype)
     if code is None:
-        _refuse(what, f"{name} is {t.dtype}, not one of float32, bfloat16, float16")
+        _refuse(what, f"{name} is {t.dtype}, not one of {', '.join(str(k)[6:] for k in types)}")
     shape = t.shape
     if not shape:
         _refuse(what, f"{name} has no dimensions")
@@ -319,9 +344,9 @@ def _rows(what, t, name, width, device=None):
     return TabxRows(t.data_ptr(), max(apart, wide), code), count
 
 
-def _same_rows(what, t, name, width, device, rows):
+def _same_rows(what, t, name, width, device, rows, types=TYPES):
     """The same for a tensor that has to have as many rows."""
-    r, n = _rows(what, t, name, width, device)
+    r, n = _rows(what, t, name, width, device, types)
     if n != rows:
         _refuse(what, f"{name} has {n} rows, not {rows}")
     return r
@@ -480,6 +505,227 @@ def tabx_action_log_prob_backward(logits, actions, temperature, grad_log_prob, g
              _needed(what, actions, "actions", rows, u8, dev), temperature,
              _array(what, grad_log_prob, "grad_log_prob", rows, f32, dev),
              _array(what, grad_entropy, "grad_entropy", rows, f32, dev), C.byref(gr))
+
+
+# --- a unit's memory ---------------------------------------------------------------------------------
+
+_E4M3, _INT = 3, 4                      # types that TYPES does not have: rows of the layer norm are none of them
+_NARROW = {**TYPES, torch.float8_e4m3fn: _E4M3}
+
+
+def tabx_rms_norm(x, weight, eps, y, scale=None, rstd=None, residual=None, sum=None, row_mask=None,
+                  stream=None):
+    """y = root-mean-square norm of the rows of x + residual (over the last dimension) whose row_mask byte is
+    not 0; the sum itself to `sum`.  y may be float8_e4m3fn, then scale [rows] takes what each row was divided by."""
+    what, f32, dev = "tabx_rms_norm", torch.float32, x.get_device()
+    xr, rows = _rows(what, x, "x", 0)
+    width = x.shape[-1]
+    yr = _same_rows(what, y, "y", width, dev, rows, _NARROW)
+    rr = sr = None
+    if residual is not None:
+        rr = C.byref(_same_rows(what, residual, "residual", width, dev, rows))
+    if sum is not None:
+        sr = C.byref(_same_rows(what, sum, "sum", width, dev, rows))
+    if (scale is None) == (yr.type == _E4M3):
+        _refuse(what, "scale goes with a y of 8 bits")
+    _enqueue(what, _lib.tabx_rms_norm, dev, stream, (sum, y, scale, rstd), rows, width, C.byref(xr), rr,
+             _array(what, row_mask, "row_mask", rows, torch.uint8, dev),
+             _array(what, weight, "weight", width, f32, dev), eps, sr, C.byref(yr),
+             _array(what, scale, "scale", rows, f32, dev), _array(what, rstd, "rstd", rows, f32, dev))
+
+
+def tabx_rms_norm_workspace(rows: int, width: int) -> int:
+    """Bytes of workspace that tabx_rms_norm_backward needs for the weight's gradient."""
+    if not (-1 <= width <= _MOST and -1 <= rows < 2 ** 63):
+        _refuse("tabx_rms_norm_workspace", f"{rows} rows of {width} elements")
+    n = _lib.tabx_rms_norm_workspace(rows, width)
+    if n < 0:
+        _check(n, "tabx_rms_norm_workspace")
+    return n
+
+
+def tabx_rms_norm_backward(sum, weight, rstd, grad_y, grad_sum=None, grad_x=None, grad_weight=None,
+                           workspace=None, row_mask=None, stream=None):
+    """The gradients of tabx_rms_norm, of the sum that it normed: grad_x is x's and the residual's.  Those
+    that are None are not computed."""
+    what, f32, dev = "tabx_rms_norm_backward", torch.float32, sum.get_device()
+    sr, rows = _rows(what, sum, "sum", 0)
+    width = sum.shape[-1]
+    gr = _same_rows(what, grad_y, "grad_y", width, dev, rows)
+    ar = ir = None
+    if grad_sum is not None:
+        ar = C.byref(_same_rows(what, grad_sum, "grad_sum", width, dev, rows))
+    if grad_x is not None:
+        ir = C.byref(_same_rows(what, grad_x, "grad_x", width, dev, rows))
+    size = 0 if workspace is None else workspace.numel()
+    _enqueue(what, _lib.tabx_rms_norm_backward, dev, stream, (grad_x, grad_weight), rows, width, C.byref(sr),
+             _array(what, row_mask, "row_mask", rows, torch.uint8, dev),
+             _array(what, weight, "weight", width, f32, dev),
+             _needed(what, rstd, "rstd", rows, f32, dev), C.byref(gr), ar, ir,
+             _array(what, grad_weight, "grad_weight", width, f32, dev),
+             _array(what, workspace, "workspace", size, torch.uint8, dev), size)
+
+
+def _heads(what, t, name, device, ticks=None):
+    """(TabxHeads, rows, heads, width) of a tensor [rows ..., heads, width], with the ticks before the
+    rows if `ticks` is given, whose rows lie at equal distances."""
+    code = TYPES.get(t.dtype)
+    if code is None:
+        _refuse(what, f"{name} is {t.dtype}, not one of float32, bfloat16, float16")
+    shape, stride = t.shape, t.stride()
+    first, n = 0 if ticks is None else 1, len(shape)
+    if n < first + 2:
+        _refuse(what, f"{name} has {n} dimensions")
+    if first and shape[0] != ticks:
+        _refuse(what, f"{name} has {shape[0]} ticks, not {ticks}")
+    if shape[-1] > _MOST or shape[-2] > _MOST:
+        _refuse(what, f"{name} has {shape[-2]} heads of {shape[-1]} elements")
+    if t.get_device() != device:
+        _elsewhere(what, t, name, device)
+    if shape[-1] > 1 and stride[-1] != 1:
+        _refuse(what, f"the elements of a head of {name} are not next to each other")
+    count, apart = 1, 0
+    for d in range(n - 3, first - 1, -1):
+        if shape[d] == 1:
+            continue
+        if count == 1:
+            apart = stride[d]
+        elif stride[d] != apart * count:
+            _refuse(what, f"the rows of {name} do not lie at equal distances")
+        count *= shape[d]
+    return (TabxHeads(t.data_ptr(), stride[0] if first and shape[0] > 1 else 0, apart,
+                      stride[-2] if shape[-2] > 1 else 0, code), count, shape[-2], shape[-1])
+
+
+def _same_heads(what, t, name, device, rows, heads, width, ticks=None):
+    """The same for a tensor of known sizes."""
+    h, n, m, w = _heads(what, t, name, device, ticks)
+    if (n, m, w) != (rows, heads, width):
+        _refuse(what, f"{name} has {n} rows of {m} heads of {w} elements, not {rows} of {heads} of {width}")
+    return h
+
+
+def tabx_rotary(x, axes, frequency, y, interleaved=False, inverse=False, row_mask=None, stream=None):
+    """y = x [rows ..., heads, width] with pairs of each head's elements turned.  axes: for each axis (position,
+    pairs), position an int32 or float32 tensor of an element per row, or per run of as many rows as there are
+    to one (an env's units); frequency: float64, an element per pair."""
+    what, dev = "tabx_rotary", x.get_device()
+    xh, rows, heads, width = _heads(what, x, "x", dev)
+    yh = _same_heads(what, y, "y", dev, rows, heads, width)
+    if not 1 <= len(axes) <= 4:
+        _refuse(what, f"{len(axes)} axes, not 1 to 4")
+    own, total = (TabxAxis * len(axes))(), 0
+    for a, (position, pairs) in zip(own, axes):
+        kind = _INT if position.dtype is torch.int32 else 0 if position.dtype is torch.float32 else None
+        if kind is None:
+            _refuse(what, f"position is {position.dtype}, not int32 or float32")
+        n = position.numel()
+        if rows and (n == 0 or rows % n or rows // n > _MOST):
+            _refuse(what, f"position has {n} elements, which does not divide {rows} rows")
+        if not 0 <= pairs <= _MOST:
+            _refuse(what, f"{pairs} pairs")
+        a.position = _array(what, position, "position", n, position.dtype, dev)
+        a.type, a.units, a.pairs = kind, rows // n if n else 1, pairs
+        total += pairs
+    _enqueue(what, _lib.tabx_rotary, dev, stream, (y,), rows, heads, width, C.byref(xh),
+             _array(what, row_mask, "row_mask", rows, torch.uint8, dev), own, len(axes),
+             _needed(what, frequency, "frequency", total, torch.float64, dev), bool(interleaved), bool(inverse),
+             C.byref(yh))
+
+
+def _flags(what, t, name, ticks, rows, device):
+    """(address, units) of bytes that stand for runs of rows, at each of `ticks` ticks."""
+    if t is None:
+        return None, 1
+    n = t.numel() // ticks if ticks else 0
+    if ticks and (n * ticks != t.numel() or (rows and (n == 0 or rows % n or rows // n > _MOST))):
+        _refuse(what, f"{name} has {t.numel()} elements, which {ticks} ticks of {rows} rows do not share")
+    return _array(what, t, name, t.numel(), torch.uint8, device), rows // n if n else 1
+
+
+def _numbered(what, heads, key, value, rows, log_decay, device):
+    if heads > _MOST:
+        _refuse(what, f"{heads} heads")
+    return _needed(what, log_decay, "log_decay", heads, torch.float32, device), rows * heads * key * value
+
+
+def tabx_linear_attention_step(q, k, v, log_decay, scale, state, out, fresh=None, controlled=None,
+                               stream=None):
+    """One tick of a memory: state [rows ..., heads, key, value] (float32, in place) fades, or is forgotten where
+    fresh says (a byte per row, or per run of rows: an env's `dones`), takes k and v in, and q reads it.
+    q, k [rows ..., heads, key], v, out [rows ..., heads, value]."""
+    what, f32, dev = "tabx_linear_attention_step", torch.float32, q.get_device()
+    qh, rows, heads, key = _heads(what, q, "q", dev)
+    kh = _same_heads(what, k, "k", dev, rows, heads, key)
+    value = v.shape[-1] if v.dim() else 0
+    vh = _same_heads(what, v, "v", dev, rows, heads, value)
+    oh = _same_heads(what, out, "out", dev, rows, heads, value)
+    decay, size = _numbered(what, heads, key, value, rows, log_decay, dev)
+    fp, units = _flags(what, fresh, "fresh", 1, rows, dev)
+    _enqueue(what, _lib.tabx_linear_attention_step, dev, stream, (state, out), rows, heads, key, value,
+             C.byref(qh), C.byref(kh), C.byref(vh), decay, scale, fp, units,
+             _array(what, controlled, "controlled", rows, torch.uint8, dev),
+             _needed(what, state, "state", size, f32, dev), C.byref(oh))
+
+
+def tabx_linear_attention_workspace(ticks: int, rows: int, heads: int, key_width: int,
+                                    value_width: int) -> int:
+    """Bytes of workspace that tabx_linear_attention and its backward pass need."""
+    small = all(-1 <= n <= _MOST for n in (heads, key_width, value_width))
+    if not (small and -1 <= ticks < 2 ** 63 and -1 <= rows < 2 ** 63):
+        _refuse("tabx_linear_attention_workspace", f"{ticks} ticks, {rows} rows, {heads} heads of {key_width} and {value_width}")
+    n = _lib.tabx_linear_attention_workspace(ticks, rows, heads, key_width, value_width)
+    if n < 0:
+        _check(n, "tabx_linear_attention_workspace")
+    return n
+
+
+def tabx_linear_attention(q, k, v, log_decay, scale, out, fresh=None, state_in=None, state_out=None,
+                          workspace=None, controlled=None, stream=None):
+    """Many ticks of a memory at once: q, k [ticks, rows ..., heads, key], v, out [ticks, rows ..., heads, value],
+    fresh [ticks, rows or runs of rows]."""
+    what, f32, dev = "tabx_linear_attention", torch.float32, q.get_device()
+    ticks = q.shape[0] if q.dim() else 0
+    qh, rows, heads, key = _heads(what, q, "q", dev, ticks)
+    kh = _same_heads(what, k, "k", dev, rows, heads, key, ticks)
+    value = v.shape[-1] if v.dim() else 0
+    vh = _same_heads(what, v, "v", dev, rows, heads, value, ticks)
+    oh = _same_heads(what, out, "out", dev, rows, heads, value, ticks)
+    decay, size = _numbered(what, heads, key, value, rows, log_decay, dev)
+    fp, units = _flags(what, fresh, "fresh", ticks, rows, dev)
+    room = 0 if workspace is None else workspace.numel()
+    _enqueue(what, _lib.tabx_linear_attention, dev, stream, (out, state_out), ticks, rows, heads, key, value,
+             C.byref(qh), C.byref(kh), C.byref(vh), decay, scale, fp, units,
+             _array(what, controlled, "controlled", rows, torch.uint8, dev),
+             _array(what, state_in, "state_in", size, f32, dev),
+             _array(what, state_out, "state_out", size, f32, dev), C.byref(oh),
+             _array(what, workspace, "workspace", room, torch.uint8, dev), room)
+
+
+def tabx_linear_attention_backward(q, k, v, log_decay, scale, grad_out, grad_q, grad_k, grad_v, fresh=None,
+                                   state_in=None, grad_state_out=None, grad_state_in=None, workspace=None,
+                                   controlled=None, stream=None):
+    """The gradients of tabx_linear_attention; those that are None are not computed."""
+    what, f32, dev = "tabx_linear_attention_backward", torch.float32, q.get_device()
+    ticks = q.shape[0] if q.dim() else 0
+    qh, rows, heads, key = _heads(what, q, "q", dev, ticks)
+    kh = _same_heads(what, k, "k", dev, rows, heads, key, ticks)
+    value = v.shape[-1] if v.dim() else 0
+    vh = _same_heads(what, v, "v", dev, rows, heads, value, ticks)
+    oh = _same_heads(what, grad_out, "grad_out", dev, rows, heads, value, ticks)
+    gradients = [None if t is None else C.byref(_same_heads(what, t, name, dev, rows, heads, width, ticks))
+                 for t, name, width in ((grad_q, "grad_q", key), (grad_k, "grad_k", key),
+                                        (grad_v, "grad_v", value))]
+    decay, size = _numbered(what, heads, key, value, rows, log_decay, dev)
+    fp, units = _flags(what, fresh, "fresh", ticks, rows, dev)
+    room = 0 if workspace is None else workspace.numel()
+    _enqueue(what, _lib.tabx_linear_attention_backward, dev, stream, (grad_q, grad_k, grad_v, grad_state_in),
+             ticks, rows, heads, key, value, C.byref(qh), C.byref(kh), C.byref(vh), decay, scale, fp, units,
+             _array(what, controlled, "controlled", rows, torch.uint8, dev),
+             _array(what, state_in, "state_in", size, f32, dev),
+             _array(what, grad_state_out, "grad_state_out", size, f32, dev), C.byref(oh), *gradients,
+             _array(what, grad_state_in, "grad_state_in", size, f32, dev),
+             _array(what, workspace, "workspace", room, torch.uint8, dev), room)
 
 
 class TabxEnv:
@@ -686,6 +932,19 @@ class TabxEnv:
             _refuse("sample_levels", f"scores has rows of {scores.shape[-1]} elements, not {levels}")
         tabx_sample_levels(scores, sampling, uniform, self.st["next_level"], level_mask, env_mask,
                            stream)
+
+    def rotate(self, x, pairs, frequency, y, interleaved=False, inverse=False, controlled=None, stream=None):
+        """y = x [E, N, heads, width] turned by the tick of each env's episode and the place of each unit as the
+        last tick left them: pairs of (t, x, y), frequency of all of them together."""
+        axes = [(self.st[name], n) for name, n in zip(("t", "x", "y"), pairs)]
+        if len(pairs) != 3:
+            _refuse("rotate", f"pairs of {len(pairs)} axes, not of t, x and y")
+        tabx_rotary(x, axes, frequency, y, interleaved, inverse, controlled, stream)
+
+    def remember(self, q, k, v, log_decay, scale, state, out, controlled=None, stream=None):
+        """One tick of the units' memory, state [E, N, heads, key, value]: forgotten where the last tick ended an
+        episode (`dones`).  After a reset of other envs the caller clears their states."""
+        tabx_linear_attention_step(q, k, v, log_decay, scale, state, out, self.dones, controlled, stream)
 
     def snapshot(self) -> dict:
         return {k: v.clone() for k, v in self.st.items()}

@@ -9,11 +9,12 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
 SOURCES = [os.path.join(_PKG, "csrc", "tabx_kernels.hip")]              # the tick
 LEARNER_SOURCES = [os.path.join(_PKG, "csrc", "tabx_learner.hip")]      # the learner's side of it
+MEMORY_SOURCES = [os.path.join(_PKG, "csrc", "tabx_memory.hip")]        # a unit's memory over its ticks
 HEADERS = [os.path.join(_ROOT, "include", "tabx.h")] + [
     os.path.join(_PKG, "csrc", h)
     for h in ("tabx_device.h", "tabx_policy.h", "tabx_step.h", "tabx_observe.h",
               "tabx_observe_packed.h", "tabx_rows.h", "tabx_teams.h", "tabx_host.h", "tabx_norm.h",
-              "tabx_sample.h", "tabx_levels.h")]
+              "tabx_sample.h", "tabx_levels.h", "tabx_rms.h", "tabx_rotary.h", "tabx_attention.h")]
 LIB_PATH = os.path.join(_PKG, "libtabx.so")
 
 HIPCC_FLAGS = [
@@ -27,7 +28,7 @@ HIPCC_FLAGS = [
 
 def build(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc] + HIPCC_FLAGS + SOURCES + LEARNER_SOURCES + ["-o", LIB_PATH]
+    cmd = [hipcc] + HIPCC_FLAGS + SOURCES + LEARNER_SOURCES + MEMORY_SOURCES + ["-o", LIB_PATH]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
@@ -38,7 +39,7 @@ def is_stale() -> bool:
     if not os.path.exists(LIB_PATH):
         return True
     t = os.path.getmtime(LIB_PATH)
-    return any(os.path.getmtime(f) > t for f in SOURCES + LEARNER_SOURCES + HEADERS)
+    return any(os.path.getmtime(f) > t for f in SOURCES + LEARNER_SOURCES + MEMORY_SOURCES + HEADERS)
 
 
 if __name__ == "__main__":

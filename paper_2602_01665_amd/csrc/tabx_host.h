@@ -16,14 +16,14 @@ static int check_rows(int64_t rows, int32_t width)
     return rows < 0 || rows > (int64_t)1 << 40 || width < 1 ? TABX_ERR_SHAPE : TABX_OK;
 }
 
-// An array of rows; NULL only where it is `optional`.
-static int check_array(const TabxRows *m, int64_t rows, int32_t width, bool optional = false)
+// An array of rows; NULL only where it is `optional`, of types up to `last`.
+static int check_array(const TabxRows *m, int64_t rows, int32_t width, bool optional = false, int32_t last = TABX_F16)
 {
     if (!m) return optional ? TABX_OK : TABX_ERR_NULL;
-    if (m->type < TABX_F32 || m->type > TABX_F16) return TABX_ERR_SHAPE;
+    if (m->type < TABX_F32 || m->type > last) return TABX_ERR_SHAPE;
     if (m->stride < width || (rows > 0 && m->stride > ((int64_t)1 << 60) / rows)) return TABX_ERR_SHAPE;
     if (!m->data) return TABX_ERR_NULL;
-    return on_boundary(m->data, m->type == TABX_F32 ? 4 : 2) ? TABX_OK : TABX_ERR_ALIGN;
+    return m->type == TABX_E4M3 || on_boundary(m->data, m->type == TABX_F32 ? 4 : 2) ? TABX_OK : TABX_ERR_ALIGN;
 }
 
 static int check_floats(const void *p, bool optional)
@@ -55,7 +55,7 @@ constexpr int64_t kMostGroups = (int64_t)1 << 20;  // of a launch; beyond them i
 
 static int64_t quotient_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 static int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
-static int64_t size_of(int type) { return type == TABX_F32 ? 4 : 2; }
+static int64_t size_of(int type) { return type == TABX_F32 ? 4 : type == TABX_E4M3 ? 1 : 2; }
 
 // Teams of a workgroup, and rows that a team works on at a time.
 constexpr int teams_of(int lanes) { return lanes <= 64 ? threads_of(lanes) / 64 : 1; }

@@ -1,0 +1,488 @@
+// A unit's memory for MI355X (gfx950): norm of the residual stream, rotation by tick and place, linear attention with a
+// decay for each head over an episode's ticks, and their gradients.
+//
+// Files: tabx_rows.h (element types, sums over lanes), tabx_teams.h (rows in registers), tabx_rms.h, tabx_rotary.h,
+// tabx_attention.h (the kernels), tabx_host.h (argument checks, launches), this file (the C entry points).  Arithmetic is
+// float32 (float64 for angles).
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "tabx.h"
+
+#pragma clang fp contract(off)
+
+#include "tabx_attention.h"
+#include "tabx_host.h"
+#include "tabx_rms.h"
+#include "tabx_rotary.h"
+
+namespace tabx {
+
+// --- root-mean-square norm ----------------------------------------------------------------------
+
+constexpr int64_t kRmsTeams = 10 * 8192;           // teams that share the rows of a forward call, if they are many
+constexpr int64_t kRmsTurns = 4;                   // turns of a team's run of rows in a backward call
+constexpr int64_t kRmsAlone = 2;                   // workgroups whose rows one takes alone in a backward call
+
+template <int LANES, int PIECES>
+struct RmsForward {
+    static constexpr bool kUsed = LANES > 32 || PIECES < 3;
+    template <int X_BYTES>
+    static int with_type(const RmsArgs &a, int64_t groups, void *stream)
+    {
+        return launch(!a.residual                     ? tabx_rms_kernel<LANES, PIECES, X_BYTES, 0>
+                      : size_of(a.residual_type) == 4 ? tabx_rms_kernel<LANES, PIECES, X_BYTES, 4>
+                                                      : tabx_rms_kernel<LANES, PIECES, X_BYTES, 2>,
+                      groups, threads_of(LANES), a, stream);
+    }
+    static int go(RmsArgs a, void *stream)
+    {
+        constexpr int teams = teams_of(LANES);
+        constexpr bool stays = LANES * PIECES > 768;
+        a.team_rows = LANES <= 64 ? least(quotient_up(quotient_up(a.rows, kRmsTeams), at_once(LANES)) * at_once(LANES), 64) : 1;
+        const int64_t groups = least(quotient_up(a.rows, a.team_rows * teams), stays ? kComputeUnits * 2048 / LANES : kMostGroups);
+        a.lap = groups * teams * a.team_rows;
+        return a.x_type == TABX_F32 ? with_type<4>(a, groups, stream) : with_type<2>(a, groups, stream);
+    }
+};
+
+template <int LANES, int PIECES>
+struct RmsGroups {
+    static constexpr bool kUsed = LANES > 32 || PIECES < 3;
+    static int go(int64_t rows)
+    {
+        constexpr int64_t most = kComputeUnits * 4 * grad_wavefronts(PIECES) * 64 / threads_of(LANES);
+        const int64_t groups = quotient_up(rows, kRmsTurns * at_once(LANES) * teams_of(LANES));
+        return (int)(groups <= kRmsAlone ? 1 : least(groups, most));
+    }
+};
+
+static int rms_groups(int64_t rows, int32_t width) { return for_width<RmsGroups>((width + 3) / 4, rows); }
+
+template <int LANES, int PIECES>
+struct RmsBackward {
+    static constexpr bool kUsed = RmsGroups<LANES, PIECES>::kUsed;
+    template <int X_BYTES, int G_BYTES>
+    static int with_types(const RmsArgs &a, int64_t groups, void *stream)
+    {
+        return launch(!a.y          ? tabx_rms_grad_kernel<LANES, PIECES, X_BYTES, G_BYTES, false, false>
+                      : a.grad_sum  ? tabx_rms_grad_kernel<LANES, PIECES, X_BYTES, G_BYTES, true, true>
+                                    : tabx_rms_grad_kernel<LANES, PIECES, X_BYTES, G_BYTES, true, false>,
+                      groups, threads_of(LANES), a, stream);
+    }
+    static int go(RmsArgs a, int64_t groups, void *stream)
+    {
+        constexpr int turns_at_once = at_once(LANES);
+        a.team_rows = least(quotient_up(quotient_up(a.rows, groups * teams_of(LANES)), turns_at_once), kRmsTurns) * turns_at_once;
+        a.team_rows = least(a.team_rows, 64);
+        a.lap = groups * teams_of(LANES) * a.team_rows;
+        if (a.x_type == TABX_F32) return a.g_type == TABX_F32 ? with_types<4, 4>(a, groups, stream) : with_types<4, 2>(a, groups, stream);
+        return a.g_type == TABX_F32 ? with_types<2, 4>(a, groups, stream) : with_types<2, 2>(a, groups, stream);
+    }
+};
+
+// Adds up the workgroups' parts: 32 columns per workgroup, 32 runs of parts side by side, always in the same order.
+static __global__ __launch_bounds__(1024) void tabx_rms_join_kernel(const float *partial, int parts, int width, float *grad_weight)
+{
+    __shared__ float meet[32][33];
+    const int c = (int)threadIdx.x & 31, run = (int)threadIdx.x >> 5;
+    const int j = (int)blockIdx.x * 32 + c;
+    float s = 0.0f;
+    if (j < width) {
+#pragma unroll 8
+        for (int k = run; k < parts; k += 32) s += partial[(int64_t)k * width + j];
+    }
+    meet[run][c] = s;
+    __syncthreads();
+    if (run != 0 || j >= width) return;
+#pragma unroll
+    for (int k = 1; k < 32; ++k) s += meet[k][c];
+    grad_weight[j] = s;
+}
+
+static int rms_join(const float *partial, int parts, int width, float *grad_weight, void *stream)
+{
+    void *args[] = {(void *)&partial, (void *)&parts, (void *)&width, (void *)&grad_weight};
+    return launched(hipLaunchKernel((const void *)tabx_rms_join_kernel, dim3((unsigned)(width + 31) / 32), dim3(1024), args, 0,
+                                    (hipStream_t)stream));
+}
+
+static int rms_backward(RmsArgs a, float *grad_weight, void *stream)
+{
+    const int64_t groups = rms_groups(a.rows, a.width);
+    if (groups == 1) {                             // its sums are the gradient
+        a.partial = nullptr;
+        a.grad_weight = grad_weight;
+    }
+    const int rc = for_width<RmsBackward>((a.width + 3) / 4, a, groups, stream);
+    return rc != TABX_OK || !a.partial ? rc : rms_join(a.partial, (int)groups, a.width, grad_weight, stream);
+}
+
+// --- heads --------------------------------------------------------------------------------------
+
+// An array of heads; with `apart`, no two of its elements may share their place.
+static int check_heads(const TabxHeads *m, int64_t ticks, int64_t rows, int32_t heads, int32_t width, bool apart)
+{
+    if (!m) return TABX_ERR_NULL;
+    if (m->type < TABX_F32 || m->type > TABX_F16) return TABX_ERR_SHAPE;
+    const int64_t count[3] = {ticks, rows, heads}, stride[3] = {m->tick_stride, m->row_stride, m->head_stride};
+    int64_t reach = width;
+    for (int k = 0; k < 3; ++k) {
+        if (count[k] <= 1) continue;
+        if (stride[k] < 0 || stride[k] > ((int64_t)1 << 60) / count[k]) return TABX_ERR_SHAPE;
+        reach += stride[k] * (count[k] - 1);
+    }
+    if (reach > (int64_t)1 << 60) return TABX_ERR_SHAPE;
+    if (apart) {
+        // from the smallest stride on, each one passes over what lies below it
+        int64_t span = width;
+        bool done[3] = {count[0] <= 1, count[1] <= 1, count[2] <= 1};
+        for (int turn = 0; turn < 3; ++turn) {
+            int k = -1;
+            for (int n = 0; n < 3; ++n)
+                if (!done[n] && (k < 0 || stride[n] < stride[k])) k = n;
+            if (k < 0) break;
+            if (stride[k] < span) return TABX_ERR_SHAPE;
+            span += stride[k] * (count[k] - 1);
+            done[k] = true;
+        }
+    }
+    if (!m->data) return TABX_ERR_NULL;
+    return on_boundary(m->data, m->type == TABX_F32 ? 4 : 2) ? TABX_OK : TABX_ERR_ALIGN;
+}
+
+static int check_units(int64_t rows, int32_t units) { return units < 1 || rows % units != 0 ? TABX_ERR_SHAPE : TABX_OK; }
+
+static Strides strides_of(const TabxHeads &m) { return Strides{m.tick_stride, m.row_stride, m.head_stride}; }
+
+// --- rotation -----------------------------------------------------------------------------------
+
+template <int LANES>
+static int launch_rotary(const RotaryArgs &a, void *stream)
+{
+    const int64_t groups = least(quotient_up(a.rows, 256 / LANES), kMostGroups);
+    return launch(a.type == TABX_F32    ? tabx_rotary_kernel<LANES, TABX_F32>
+                  : a.type == TABX_BF16 ? tabx_rotary_kernel<LANES, TABX_BF16>
+                                        : tabx_rotary_kernel<LANES, TABX_F16>,
+                  groups, 256, a, stream);
+}
+
+// --- linear attention ---------------------------------------------------------------------------
+
+// Sizes that the calls have in common; a call of no rows is fine.
+static int check_attention(int64_t ticks, int64_t rows, int32_t heads, int32_t keys, int32_t values)
+{
+    if (ticks < 0 || ticks > (int64_t)1 << 30 || rows < 0 || heads < 1 || heads > TABX_ATTENTION_MAX_HEADS) return TABX_ERR_SHAPE;
+    if (rows > INT32_MAX / heads) return TABX_ERR_SHAPE;
+    if (keys < 1 || keys > TABX_ATTENTION_MAX_WIDTH || values < 1 || values > TABX_ATTENTION_MAX_WIDTH) return TABX_ERR_SHAPE;
+    return TABX_OK;
+}
+
+// Into how many segments of how many ticks a row's ticks are cut: where there are few rows and heads, so many that
+// the machine has something to do, each of several chunks.
+struct Segments {
+    int64_t count, ticks;
+};
+constexpr int64_t kSegmentTicks = 128;             // at least; a multiple of every chunk
+constexpr int64_t kSegmentWorks = 1024;            // of the whole call, about
+
+static Segments segments_of(int64_t ticks, int64_t rows, int32_t heads)
+{
+    const int64_t works = rows * heads;
+    int64_t most = works > 0 ? kSegmentWorks / works : 1;
+    if (most < 1) most = 1;
+    int64_t length = quotient_up(quotient_up(ticks, most), kSegmentTicks) * kSegmentTicks;
+    if (length < kSegmentTicks) length = kSegmentTicks;
+    const int64_t count = quotient_up(ticks, length);
+    return Segments{count < 1 ? 1 : count, length};
+}
+
+static int64_t attention_workspace(int64_t ticks, int64_t rows, int32_t heads, int32_t keys, int32_t values)
+{
+    const Segments s = segments_of(ticks, rows, heads);
+    return s.count == 1 ? 0 : rows * heads * s.count * ((int64_t)keys * values + 1) * (int64_t)sizeof(float);
+}
+
+template <int D, bool CARRY>
+static int launch_attention(const AttentionArgs &a, void *stream)
+{
+    return launch(tabx_attention_kernel<D, CARRY>, least(a.works, kMostGroups), D >= 64 ? 256 : 4 * D, a, stream);
+}
+
+template <bool CARRY>
+static int attention_of_width(const AttentionArgs &a, void *stream)
+{
+    const int width = a.keys > a.values ? a.keys : a.values;
+    if (width <= 16) return launch_attention<16, CARRY>(a, stream);
+    if (width <= 32) return launch_attention<32, CARRY>(a, stream);
+    if (width <= 64) return launch_attention<64, CARRY>(a, stream);
+    return launch_attention<128, CARRY>(a, stream);
+}
+
+static int attention(AttentionArgs a, void *workspace, void *stream)
+{
+    const Segments s = segments_of(a.ticks, a.rows, a.heads);
+    a.segments = (int32_t)s.count;
+    a.segment = s.ticks;
+    a.works = a.rows * a.heads * s.count;
+    a.envs = a.rows / a.units;
+    if (s.count > 1) {
+        a.carried = (float *)workspace;
+        a.kept = a.carried + a.works * a.keys * a.values;
+        int rc = attention_of_width<true>(a, stream);
+        if (rc) return rc;
+        const int64_t states = a.rows * a.heads * a.keys * a.values;
+        if ((rc = launch(tabx_attention_join_kernel, least(quotient_up(states, 256), kMostGroups), 256, a, stream))) return rc;
+    }
+    return attention_of_width<false>(a, stream);
+}
+
+static int check_workspace(const void *workspace, int64_t bytes, int64_t needed)
+{
+    if (needed == 0) return TABX_OK;
+    if (!workspace) return TABX_ERR_NULL;
+    if (!on_boundary(workspace, 16)) return TABX_ERR_ALIGN;
+    return bytes < needed ? TABX_ERR_SHAPE : TABX_OK;
+}
+
+// q, k and v of one type, and one that is written or read beside them.
+static int check_inputs(int64_t ticks, int64_t rows, int32_t heads, int32_t keys, int32_t values, const TabxHeads *q,
+                        const TabxHeads *k, const TabxHeads *v, const TabxHeads *out, bool written)
+{
+    int rc;
+    if ((rc = check_heads(q, ticks, rows, heads, keys, false)) || (rc = check_heads(k, ticks, rows, heads, keys, false))) return rc;
+    if ((rc = check_heads(v, ticks, rows, heads, values, false)) || (rc = check_heads(out, ticks, rows, heads, values, written))) return rc;
+    return q->type == k->type && q->type == v->type && q->type == out->type ? TABX_OK : TABX_ERR_SHAPE;
+}
+
+} // namespace tabx
+
+extern "C" {
+
+int tabx_rms_norm(int64_t rows, int32_t width, const TabxRows *x, const TabxRows *residual, const uint8_t *row_mask,
+                  const float *weight, float eps, const TabxRows *sum, const TabxRows *y, float *scale, float *rstd, void *stream)
+{
+    using namespace tabx;
+    int rc = check_rows(rows, width);
+    if (rc) return rc;
+    if (width > TABX_NORM_MAX_WIDTH) return TABX_ERR_SHAPE;
+    if (!(eps >= 0.0f && eps < INFINITY)) return TABX_ERR_PARAM;
+    if (rows == 0) return TABX_OK;
+    if ((rc = check_array(x, rows, width)) || (rc = check_array(residual, rows, width, true))) return rc;
+    if ((rc = check_array(sum, rows, width, true)) || (rc = check_array(y, rows, width, false, TABX_E4M3))) return rc;
+    if ((rc = check_floats(weight, true)) || (rc = check_floats(scale, y->type != TABX_E4M3)) || (rc = check_floats(rstd, true))) return rc;
+    if (scale && y->type != TABX_E4M3) return TABX_ERR_SHAPE;
+    RmsArgs a = {};
+    a.x = x->data, a.x_stride = x->stride, a.x_type = x->type;
+    if (residual) a.residual = residual->data, a.residual_stride = residual->stride, a.residual_type = residual->type;
+    if (sum) a.sum = sum->data, a.sum_stride = sum->stride, a.sum_type = sum->type;
+    a.y = y->data, a.y_stride = y->stride, a.y_type = y->type;
+    a.row_mask = row_mask;
+    a.weight = weight, a.scale = scale, a.rstd = rstd;
+    a.rows = rows, a.width = width, a.eps = eps, a.inv_width = 1.0f / (float)width;
+    return for_width<RmsForward>((width + 3) / 4, a, stream);
+}
+
+int64_t tabx_rms_norm_workspace(int64_t rows, int32_t width)
+{
+    const int rc = tabx::check_rows(rows, width);
+    if (rc || width > TABX_NORM_MAX_WIDTH) return TABX_ERR_SHAPE;
+    return (int64_t)tabx::rms_groups(rows, width) * width * (int64_t)sizeof(float);
+}
+
+int tabx_rms_norm_backward(int64_t rows, int32_t width, const TabxRows *sum, const uint8_t *row_mask, const float *weight,
+                           const float *rstd, const TabxRows *grad_y, const TabxRows *grad_sum, const TabxRows *grad_x,
+                           float *grad_weight, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    using namespace tabx;
+    int rc = check_rows(rows, width);
+    if (rc) return rc;
+    if (width > TABX_NORM_MAX_WIDTH) return TABX_ERR_SHAPE;
+    if (rows == 0) {                               // sums over no rows
+        if ((rc = check_floats(grad_weight, true))) return rc;
+        return grad_weight ? rms_join(nullptr, 0, width, grad_weight, stream) : TABX_OK;
+    }
+    if ((rc = check_array(sum, rows, width)) || (rc = check_array(grad_y, rows, width))) return rc;
+    if ((rc = check_array(grad_sum, rows, width, true)) || (rc = check_array(grad_x, rows, width, true))) return rc;
+    if (grad_sum && grad_sum->type != sum->type) return TABX_ERR_SHAPE;
+    if ((rc = check_floats(weight, true)) || (rc = check_floats(rstd, false)) || (rc = check_floats(grad_weight, true))) return rc;
+    if (!grad_weight && !grad_x) return TABX_ERR_NULL;
+    if (grad_weight && (rc = check_workspace(workspace, workspace_bytes, tabx_rms_norm_workspace(rows, width)))) return rc;
+    RmsArgs a = {};
+    a.x = sum->data, a.x_stride = sum->stride, a.x_type = sum->type;
+    a.grad_y = grad_y->data, a.g_stride = grad_y->stride, a.g_type = grad_y->type;
+    if (grad_sum) a.grad_sum = grad_sum->data, a.grad_sum_stride = grad_sum->stride;
+    if (grad_x) a.y = grad_x->data, a.y_stride = grad_x->stride, a.y_type = grad_x->type;
+    a.row_mask = row_mask;
+    a.weight = weight, a.rstd = (float *)rstd;
+    a.partial = grad_weight ? (float *)workspace : nullptr;
+    a.rows = rows, a.width = width, a.inv_width = 1.0f / (float)width;
+    return rms_backward(a, grad_weight, stream);
+}
+
+int tabx_rotary(int64_t rows, int32_t heads, int32_t width, const TabxHeads *x, const uint8_t *row_mask, const TabxAxis *axes,
+                int32_t num_axes, const double *frequency, int32_t interleaved, int32_t inverse, const TabxHeads *y, void *stream)
+{
+    using namespace tabx;
+    if (rows < 0 || rows > (int64_t)1 << 40 || heads < 1 || width < 2 || width > TABX_ROTARY_MAX_WIDTH) return TABX_ERR_SHAPE;
+    if (num_axes < 1 || num_axes > TABX_ROTARY_MAX_AXES) return TABX_ERR_SHAPE;
+    if (!axes) return TABX_ERR_NULL;
+    RotaryArgs a = {};
+    for (int n = 0; n < num_axes; ++n) {
+        if (axes[n].pairs < 0 || axes[n].pairs > width / 2 - a.pairs) return TABX_ERR_SHAPE;
+        if (axes[n].type != TABX_F32 && axes[n].type != TABX_I32) return TABX_ERR_SHAPE;
+        if (check_units(rows, axes[n].units)) return TABX_ERR_SHAPE;
+        a.pairs += axes[n].pairs;
+        a.end[n] = a.pairs;
+        a.units[n] = axes[n].units;
+        a.axis_type[n] = axes[n].type;
+        a.position[n] = axes[n].position;
+    }
+    if (a.pairs < 1) return TABX_ERR_SHAPE;
+    if (rows == 0) return TABX_OK;
+    int rc;
+    for (int n = 0; n < num_axes; ++n)
+        if ((rc = check_floats(axes[n].position, false))) return rc;
+    if ((rc = check_heads(x, 1, rows, heads, width, false)) || (rc = check_heads(y, 1, rows, heads, width, true))) return rc;
+    if (x->type != y->type) return TABX_ERR_SHAPE;
+    if (!frequency) return TABX_ERR_NULL;
+    if (!on_boundary(frequency, 8)) return TABX_ERR_ALIGN;
+    a.x = x->data, a.x_row = x->row_stride, a.x_head = x->head_stride;
+    a.y = y->data, a.y_row = y->row_stride, a.y_head = y->head_stride;
+    a.row_mask = row_mask;
+    a.frequency = frequency;
+    a.rows = rows, a.heads = heads, a.width = width, a.type = x->type;
+    a.num_axes = num_axes, a.interleaved = interleaved != 0, a.sign = inverse ? -1.0 : 1.0;
+    a.copies = x->data != y->data;
+    const int lanes = (a.pairs + 3) / 4;
+    if (lanes <= 4) return launch_rotary<4>(a, stream);
+    if (lanes <= 8) return launch_rotary<8>(a, stream);
+    if (lanes <= 16) return launch_rotary<16>(a, stream);
+    if (lanes <= 32) return launch_rotary<32>(a, stream);
+    return launch_rotary<64>(a, stream);
+}
+
+int tabx_linear_attention_step(int64_t rows, int32_t heads, int32_t key_width, int32_t value_width, const TabxHeads *q,
+                               const TabxHeads *k, const TabxHeads *v, const float *log_decay, float scale, const uint8_t *fresh,
+                               int32_t units, const uint8_t *controlled, float *state, const TabxHeads *out, void *stream)
+{
+    using namespace tabx;
+    int rc = check_attention(1, rows, heads, key_width, value_width);
+    if (rc || (rc = check_units(rows, units))) return rc;
+    if (!(fabsf(scale) < INFINITY)) return TABX_ERR_PARAM;
+    if (rows == 0) return TABX_OK;
+    if ((rc = check_inputs(1, rows, heads, key_width, value_width, q, k, v, out, true))) return rc;
+    if ((rc = check_floats(log_decay, false)) || (rc = check_floats(state, false))) return rc;
+    StepArgs a = {};
+    a.q = q->data, a.k = k->data, a.v = v->data, a.out = out->data;
+    a.qs = strides_of(*q), a.ks = strides_of(*k), a.vs = strides_of(*v), a.os = strides_of(*out);
+    a.log_decay = log_decay, a.fresh = fresh, a.controlled = controlled;
+    a.state = state;
+    a.works = rows * heads, a.heads = heads, a.units = units, a.keys = key_width, a.values = value_width;
+    a.type = q->type, a.scale = scale;
+    const int64_t groups = least(quotient_up(a.works, 4), kMostGroups);
+    if (value_width <= 16) return launch(tabx_attention_step_kernel<16>, groups, 256, a, stream);
+    if (value_width <= 32) return launch(tabx_attention_step_kernel<32>, groups, 256, a, stream);
+    return launch(tabx_attention_step_kernel<64>, groups, 256, a, stream);
+}
+
+int64_t tabx_linear_attention_workspace(int64_t ticks, int64_t rows, int32_t heads, int32_t key_width, int32_t value_width)
+{
+    const int rc = tabx::check_attention(ticks, rows, heads, key_width, value_width);
+    return rc ? rc : tabx::attention_workspace(ticks, rows, heads, key_width, value_width);
+}
+
+int tabx_linear_attention(int64_t ticks, int64_t rows, int32_t heads, int32_t key_width, int32_t value_width, const TabxHeads *q,
+                          const TabxHeads *k, const TabxHeads *v, const float *log_decay, float scale, const uint8_t *fresh,
+                          int32_t units, const uint8_t *controlled, const float *state_in, float *state_out, const TabxHeads *out,
+                          void *workspace, int64_t workspace_bytes, void *stream)
+{
+    using namespace tabx;
+    int rc = check_attention(ticks, rows, heads, key_width, value_width);
+    if (rc || (rc = check_units(rows, units))) return rc;
+    if (!(fabsf(scale) < INFINITY)) return TABX_ERR_PARAM;
+    if (rows == 0 || (ticks == 0 && !state_out)) return TABX_OK;
+    if (ticks > 0 && (rc = check_inputs(ticks, rows, heads, key_width, value_width, q, k, v, out, true))) return rc;
+    if ((rc = check_floats(log_decay, false)) || (rc = check_floats(state_in, true)) || (rc = check_floats(state_out, true))) return rc;
+    if ((rc = check_workspace(workspace, workspace_bytes, attention_workspace(ticks, rows, heads, key_width, value_width)))) return rc;
+    AttentionArgs a = {};
+    if (ticks > 0) {
+        a.q = q->data, a.k = k->data, a.v = v->data, a.out = out->data;
+        a.qs = strides_of(*q), a.ks = strides_of(*k), a.vs = strides_of(*v), a.os = strides_of(*out);
+        a.type = q->type;
+    }
+    a.log_decay = log_decay, a.fresh = fresh, a.controlled = controlled;
+    a.state_in = state_in, a.state_out = state_out, a.state_key = value_width, a.state_value = 1;
+    a.ticks = ticks, a.rows = rows, a.heads = heads, a.units = units, a.keys = key_width, a.values = value_width;
+    a.scale_within = a.scale_state = scale, a.scale_added = 1.0f;
+    return attention(a, workspace, stream);
+}
+
+int tabx_linear_attention_backward(int64_t ticks, int64_t rows, int32_t heads, int32_t key_width, int32_t value_width,
+                                   const TabxHeads *q, const TabxHeads *k, const TabxHeads *v, const float *log_decay, float scale,
+                                   const uint8_t *fresh, int32_t units, const uint8_t *controlled, const float *state_in,
+                                   const float *grad_state_out, const TabxHeads *grad_out, const TabxHeads *grad_q,
+                                   const TabxHeads *grad_k, const TabxHeads *grad_v, float *grad_state_in, void *workspace,
+                                   int64_t workspace_bytes, void *stream)
+{
+    using namespace tabx;
+    int rc = check_attention(ticks, rows, heads, key_width, value_width);
+    if (rc || (rc = check_units(rows, units))) return rc;
+    if (!(fabsf(scale) < INFINITY)) return TABX_ERR_PARAM;
+    if (!grad_q && !grad_k && !grad_v && !grad_state_in) return TABX_ERR_NULL;
+    if (rows == 0 || (ticks == 0 && !grad_state_in)) return TABX_OK;
+    if (ticks > 0) {
+        if ((rc = check_inputs(ticks, rows, heads, key_width, value_width, q, k, v, grad_out, false))) return rc;
+        const TabxHeads *const written[3] = {grad_q, grad_k, grad_v};
+        for (int n = 0; n < 3; ++n) {
+            if (!written[n]) continue;
+            if ((rc = check_heads(written[n], ticks, rows, heads, n < 2 ? key_width : value_width, true))) return rc;
+            if (written[n]->type != q->type) return TABX_ERR_SHAPE;
+        }
+    }
+    if ((rc = check_floats(log_decay, false)) || (rc = check_floats(state_in, true)) || (rc = check_floats(grad_state_out, true)) ||
+        (rc = check_floats(grad_state_in, true)))
+        return rc;
+    if ((rc = check_workspace(workspace, workspace_bytes, attention_workspace(ticks, rows, heads, key_width, value_width)))) return rc;
+    AttentionArgs b = {};
+    b.log_decay = log_decay, b.fresh = fresh, b.controlled = controlled;
+    b.ticks = ticks, b.rows = rows, b.heads = heads, b.units = units;
+    b.zero_out = 1;
+    if (ticks > 0) b.type = q->type;
+    const auto with = [&](AttentionArgs &a, const TabxHeads *x, const TabxHeads *y, const TabxHeads *z, const TabxHeads *out, int32_t keys,
+                          int32_t values) {
+        a.keys = keys, a.values = values;
+        if (ticks > 0) {
+            a.q = x->data, a.k = y->data, a.v = z->data;
+            a.qs = strides_of(*x), a.ks = strides_of(*y), a.vs = strides_of(*z);
+            if (out) a.out = out->data, a.os = strides_of(*out);
+        }
+    };
+    if (ticks > 0 && grad_q) {                     // values are the keys, and the state lies transposed
+        AttentionArgs a = b;
+        with(a, grad_out, v, k, grad_q, value_width, key_width);
+        a.state_in = state_in, a.state_key = 1, a.state_value = value_width;
+        a.scale_within = a.scale_state = scale, a.scale_added = 1.0f;
+        if ((rc = attention(a, workspace, stream))) return rc;
+    }
+    b.backward = 1;
+    b.state_in = grad_state_out;
+    b.scale_within = scale, b.scale_state = 1.0f, b.scale_added = scale;
+    if (ticks > 0 && grad_k) {
+        AttentionArgs a = b;
+        with(a, v, grad_out, q, grad_k, value_width, key_width);
+        a.state_key = 1, a.state_value = value_width;
+        if ((rc = attention(a, workspace, stream))) return rc;
+    }
+    if (grad_v || grad_state_in) {
+        AttentionArgs a = b;
+        with(a, k, q, grad_out, grad_v, key_width, value_width);
+        a.state_key = value_width, a.state_value = 1;
+        a.state_out = grad_state_in;
+        if ((rc = attention(a, workspace, stream))) return rc;
+    }
+    return TABX_OK;
+}
+
+} // extern "C"
