@@ -114,204 +114,467 @@ __global__ __launch_bounds__(256) void tabx_attention_step_kernel(const StepArgs
 
 // --- many ticks ---------------------------------------------------------------------------------
 
-constexpr int kChunk = 32;
+// The products run in the matrix cores in bf16 with sums in 32 bits, where every 32-bit operand stands as the sum of parts
+// of 8 bits each: bf16 inputs are one part, f16 ones two (both exact), f32 ones three; what lies between (the products of
+// queries and keys, the state, the faded values) is cut into two parts, three for f32.  Of the parts' products those are taken
+// that are above the last part's own rounding, so that 2^-16 of a term is lost, 2^-23 for f32 (a term's rounding to the
+// output is 2^-8, 2^-11, 2^-24), and nothing can leave the range of 32 bits that 32 bits would hold.
+template <int TYPE> struct Parts {
+    static constexpr int in = TYPE == TABX_BF16 ? 1 : TYPE == TABX_F16 ? 2 : 3;
+    static constexpr int mid = TYPE == TABX_F32 ? 3 : 2;
+};
 
-// A workgroup has a row's head, or a segment of its ticks, and goes through the chunks with the state in registers.  Its
-// wavefronts share out the values: each holds all of the state's lines of 16 (or 32) of them, in the layout in which a
-// product leaves its result (a lane has four lines of one column), which is that of a right operand of the next product:
-// the state goes into the matrix cores as it is.  Products are of 32 bits (16 x 16 x 4): a lane's element s of four
-// consecutive ones is that of step s, on both sides.  D: keys and values, filled up with zeros.
-template <int D, bool CARRY>
-__global__ __launch_bounds__(D >= 64 ? 256 : 4 * D) void tabx_attention_kernel(const AttentionArgs a)
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int chunk_of(int type) { return type == TABX_BF16 ? 64 : 32; }
+
+template <int N>
+__device__ __forceinline__ void split(bf16x4 (&part)[N], f32x4 v)
 {
-    constexpr int C = kChunk, WAVES = D >= 64 ? 4 : D / 16, THREADS = 64 * WAVES;
-    constexpr int TILES = D / 16, MINE = TILES / WAVES;        // tiles of 16 keys; of 16 values, and this wavefront's of them
-    constexpr int WIDE = D + 4, LONG = C + 4;
-    __shared__ float qs[C][WIDE], ks[C][WIDE], kt[D][LONG], vt[D][LONG], within[C][LONG];
-    __shared__ uint32_t wild[2];                               // of this chunk and the one before: ticks with values that are not finite
+#pragma unroll
+    for (int p = 0; p < N; ++p) {
+        part[p] = __builtin_convertvector(v, bf16x4);
+        if (p + 1 < N) v -= __builtin_convertvector(part[p], f32x4);
+    }
+}
+
+__device__ __forceinline__ bf16x8 join(bf16x4 a, bf16x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
+
+// One product of operands in parts, the smallest parts' first.
+template <int NA, int NB>
+__device__ __forceinline__ f32x4 multiply(const bf16x8 (&a)[NA], const bf16x8 (&b)[NB], f32x4 c)
+{
+    constexpr int last = NA > NB ? NA : NB;
+#pragma unroll
+    for (int s = last - 1; s >= 0; --s)
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+            if (s - i >= 0 && s - i < NB) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[s - i], c, 0, 0, 0);
+    return c;
+}
+
+// Eight elements of a row as they lie in memory.
+template <int TYPE> struct Eight { u32x4 v[TYPE == TABX_F32 ? 2 : 1]; };
+
+template <int TYPE>
+__device__ __forceinline__ void load_eight(Eight<TYPE> &e, const void *data, int64_t at, int count)
+{
+    typedef typename Element<TYPE>::one T;
+    typedef u32x4 Anywhere __attribute__((aligned(2)));
+    const T *from = (const T *)data + at;
+#pragma unroll
+    for (int n = 0; n < (TYPE == TABX_F32 ? 2 : 1); ++n) e.v[n] = u32x4{0, 0, 0, 0};
+    if (count >= 8) {
+#pragma unroll
+        for (int n = 0; n < (TYPE == TABX_F32 ? 2 : 1); ++n) e.v[n] = ((const Anywhere *)from)[n];
+    } else if (count > 0) {                        // a width that is no multiple of eight
+#pragma unroll
+        for (int i = 0; i < 7; ++i) {
+            if (i >= count) continue;
+            if constexpr (TYPE == TABX_F32) e.v[i / 4][i % 4] = ((const uint32_t *)from)[i];
+            else e.v[0][i / 2] |= (uint32_t)((const uint16_t *)from)[i] << 16 * (i % 2);
+        }
+    }
+}
+
+// Not 0 in a bit of its own if one of them is not finite (an exponent of ones carries).
+template <int TYPE>
+__device__ __forceinline__ uint32_t not_finite(const Eight<TYPE> &e)
+{
+    constexpr uint32_t exponent = TYPE == TABX_F32 ? 0x7f800000u : TYPE == TABX_BF16 ? 0x7f807f80u : 0x7c007c00u;
+    constexpr uint32_t one = TYPE == TABX_F32 ? 0x00800000u : TYPE == TABX_BF16 ? 0x00800080u : 0x04000400u;
+    uint32_t found = 0;
+#pragma unroll
+    for (int n = 0; n < (TYPE == TABX_F32 ? 2 : 1); ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) found |= (e.v[n][i] & exponent) + one;
+    return found & (TYPE == TABX_F32 ? 0x80000000u : 0x80008000u);
+}
+
+// A chunk's rows of one array in LDS, a tile for each part.  Rows lie D + 8 elements apart: eight of them, of 16 bytes
+// each, or four of 32, meet all banks once.
+template <int D, int C, int PARTS>
+struct Tile {
+    static constexpr int kRow = D + 8, kPart = C * kRow;
+    __bf16 at[PARTS * kPart];
+
+    template <int TYPE>
+    __device__ __forceinline__ void put(int row, int d, const Eight<TYPE> &e)
+    {
+        if constexpr (TYPE == TABX_BF16) {
+            *(u32x4 *)&at[row * kRow + d] = e.v[0];
+        } else {
+            f32x4 v[2];
+            if constexpr (TYPE == TABX_F32) {
+                __builtin_memcpy(&v, &e.v, sizeof v);
+            } else {
+                f16x4 h[2];
+                __builtin_memcpy(&h, &e.v, sizeof h);
+                v[0] = __builtin_convertvector(h[0], f32x4), v[1] = __builtin_convertvector(h[1], f32x4);
+            }
+            bf16x4 a[PARTS], b[PARTS];
+            split(a, v[0]);
+            split(b, v[1]);
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) *(bf16x8 *)&at[p * kPart + row * kRow + d] = join(a[p], b[p]);
+        }
+    }
+    // An operand of a product over the elements of rows: row `row + col` of 16, elements from + 8 quad .. + 7.
+    __device__ __forceinline__ void along(bf16x8 (&x)[PARTS], int row, int from, int col, int quad) const
+    {
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) x[p] = *(const bf16x8 *)&at[p * kPart + (row + col) * kRow + from + 8 * quad];
+    }
+    // The same in the order in which a product leaves its results: elements from + 4 quad .. + 3 and those 16 on.
+    __device__ __forceinline__ void along_results(bf16x8 (&x)[PARTS], int row, int from, int col, int quad) const
+    {
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+            const __bf16 *const e = &at[p * kPart + (row + col) * kRow + from + 4 * quad];
+            x[p] = join(*(const bf16x4 *)e, *(const bf16x4 *)(e + 16));
+        }
+    }
+    // An operand of a product over rows: element `from + col` of rows row + 4 quad .. + 3 and those 16 on.  Sixteen
+    // lanes read four rows' sixteen elements and change them round.
+    __device__ __forceinline__ void across(bf16x8 (&x)[PARTS], int row, int from, int col, int quad) const
+    {
+        typedef s16x4 __attribute__((address_space(3))) *Lds;
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+            const __bf16 *const e = &at[p * kPart + (row + 4 * quad + col / 4) * kRow + from + 4 * (col % 4)];
+            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)e), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(e + 16 * kRow));
+            x[p] = join(__builtin_bit_cast(bf16x4, a), __builtin_bit_cast(bf16x4, b));
+        }
+    }
+};
+
+// One row's head (or a segment of its ticks) as an attention goes through it, and which way.
+struct Course {
+    int64_t ticks, begin;          // of all; where the chunk at hand begins, counted in the direction of time taken
+    int     backward;
+    __device__ __forceinline__ int64_t tick(int i) const { return backward ? ticks - 1 - (begin + i) : begin + i; }
+};
+
+template <int D, int TYPE>
+struct Attention {
+    static constexpr int C = chunk_of(TYPE), IN = Parts<TYPE>::in, MID = Parts<TYPE>::mid;
+    static constexpr int WAVES = D / 16, THREADS = 64 * WAVES, PASSES = C * D / 8 / THREADS, TILES = D / 16;
+    typedef Tile<D, C, IN> In;
+    static constexpr int kWithin = C + 8;          // distance of rows of the products of queries and keys
+
+    // A wavefront has 16 of the values and all of the state's lines of them, in the layout in which a product leaves its
+    // result (a lane has four lines of one column), which is that of an operand of the next one (`along_results`).
+    typedef f32x4 State[TILES];
+
+    struct Rows { Eight<TYPE> e[PASSES]; };
+
+    static __device__ __forceinline__ void load(Rows &rows, const void *data, int64_t at, int64_t tick, const Course &c, int n, int width)
+    {
+        constexpr int across = D / 8;
+        const int d = 8 * ((int)threadIdx.x % across);
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+            const int i = p * (THREADS / across) + (int)threadIdx.x / across;
+            load_eight<TYPE>(rows.e[p], data, at + c.tick(i < n ? i : 0) * tick + d, i < n ? width - d : 0);
+        }
+    }
+    static __device__ __forceinline__ uint32_t store(In &tile, const Rows &rows)
+    {
+        constexpr int across = D / 8;
+        uint32_t found = 0;
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+            tile.template put<TYPE>(p * (THREADS / across) + (int)threadIdx.x / across, 8 * ((int)threadIdx.x % across), rows.e[p]);
+            found |= not_finite<TYPE>(rows.e[p]);
+        }
+        return found;
+    }
+
+    // Products of queries and keys, faded by the ticks between them, 0 where they do not belong together, in parts:
+    // tiles of 16 x 16 on and below the diagonal, dealt to the wavefronts.  Rows are queries; along them the keys lie in the
+    // order of `along_results`, so that a lane's eight are next to each other.
+    static __device__ __forceinline__ void compare(__bf16 (&within)[MID][C * kWithin], const In &q, const In &k, uint64_t begins, float l2,
+                                                   float scale, int wave, int col, int quad)
+    {
+        constexpr int tiles = C / 16 * (C / 16 + 1) / 2;
+        for (int tile = wave; tile < tiles; tile += WAVES) {
+            const int I = tile < 1 ? 0 : tile < 3 ? 1 : tile < 6 ? 2 : 3, J = tile - I * (I + 1) / 2;
+            f32x4 p = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int s = 0; s < D / 32; ++s) {
+                bf16x8 x[IN], y[IN];
+                k.along(x, 16 * J, 32 * s, col, quad);
+                q.along(y, 16 * I, 32 * s, col, quad);
+                p = multiply(x, y, p);
+            }
+            const int i = 16 * I + col;
+            const uint64_t up = begins & ((2ull << i) - 1);            // episodes begun up to the query's tick
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int j = 16 * J + 4 * quad + r;
+                const bool same = j <= i && (up >> j) <= 1;            // none of them behind the key's
+                p[r] = same ? p[r] * (__builtin_amdgcn_exp2f(l2 * (float)(i - j)) * scale) : 0.0f;
+            }
+            bf16x4 part[MID];
+            split(part, p);
+            const int at = i * kWithin + 32 * (J / 2) + 8 * quad + 4 * (J % 2);
+#pragma unroll
+            for (int m = 0; m < MID; ++m) {
+                *(bf16x4 *)&within[m][at] = part[m];
+                if (I == J && I % 2 == 0) *(u32x2 *)&within[m][at + 4] = u32x2{0, 0};
+            }
+        }
+    }
+
+    // What a chunk's queries read, and the state behind the chunk.
+    template <bool READS>
+    static __device__ __forceinline__ void advance(State &state, const __bf16 (&within)[MID][C * kWithin], const In &q, const In &k, const In &v,
+                                                   uint64_t begins, int n, float l2, const AttentionArgs &a, const Course &c, int64_t out_at,
+                                                   int wave, int col, int quad)
+    {
+        bf16x8 values[C / 32][IN];                 // this lane's: 8 ticks of its column, of every 32
+#pragma unroll
+        for (int b = 0; b < C / 32; ++b) v.across(values[b], 32 * b, 16 * wave, col, quad);
+        if constexpr (READS) {
+            bf16x8 held[D / 32][MID];
+#pragma unroll
+            for (int s = 0; s < D / 32; ++s) {
+                bf16x4 x[MID], y[MID];
+                split(x, state[2 * s]);
+                split(y, state[2 * s + 1]);
+#pragma unroll
+                for (int m = 0; m < MID; ++m) held[s][m] = join(x[m], y[m]);
+            }
+#pragma unroll
+            for (int I = 0; I < C / 16; ++I) {
+                if (16 * I >= n) break;
+                const int i = 16 * I + col;
+                f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int s = 0; s < D / 32; ++s) {
+                    bf16x8 x[IN];
+                    q.along_results(x, 16 * I, 32 * s, col, quad);
+                    o = multiply(held[s], x, o);
+                }
+                const float fade = __builtin_amdgcn_exp2f(l2 * (float)(i + 1 - a.backward)) * a.scale_state;
+                const bool none = (begins & ((2ull << i) - 1)) != 0;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[r] = none ? 0.0f : o[r] * fade;
+#pragma unroll
+                for (int b = 0; b <= I / 2; ++b) {
+                    bf16x8 x[MID];
+#pragma unroll
+                    for (int m = 0; m < MID; ++m) x[m] = *(const bf16x8 *)&within[m][i * kWithin + 32 * b + 8 * quad];
+                    o = multiply(values[b], x, o);
+                }
+                const int d = 16 * wave + 4 * quad;
+                if (a.out && i < n && d < a.values) {
+                    typename Element<TYPE>::one *const to = (typename Element<TYPE>::one *)a.out + out_at + c.tick(i) * a.os.tick + d;
+                    if (d + 4 <= a.values) {
+                        store_four<TYPE>(to, o);
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 3; ++r)
+                            if (d + r < a.values) to[r] = (typename Element<TYPE>::one)o[r];
+                    }
+                }
+            }
+        }
+        // the values faded by the ticks behind theirs; those of episodes that have ended count no more
+        const int newest = begins ? 63 - __builtin_clzll(begins) : 0;
+        const float left = __builtin_amdgcn_exp2f(l2 * (float)n);
+        bf16x8 faded[C / 32][MID];
+#pragma unroll
+        for (int b = 0; b < C / 32; ++b) {
+            bf16x4 part[2][MID];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int p = IN - 1; p >= 0; --p) {
+                    const bf16x4 y = half ? __builtin_shufflevector(values[b][p], values[b][p], 4, 5, 6, 7)
+                                          : __builtin_shufflevector(values[b][p], values[b][p], 0, 1, 2, 3);
+                    x += __builtin_convertvector(y, f32x4);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int j = 32 * b + 16 * half + 4 * quad + r;
+                    x[r] = j >= newest && j < n ? x[r] * (__builtin_amdgcn_exp2f(l2 * (float)(n - 1 - j + a.backward)) * a.scale_added) : 0.0f;
+                }
+                split(part[half], x);
+            }
+#pragma unroll
+            for (int m = 0; m < MID; ++m) faded[b][m] = join(part[0][m], part[1][m]);
+        }
+#pragma unroll
+        for (int s = 0; s < TILES; ++s) {
+            f32x4 x;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] = begins ? 0.0f : state[s][r] * left;
+#pragma unroll
+            for (int b = 0; b < C / 32; ++b) {
+                if (32 * b >= n) break;
+                bf16x8 y[IN];
+                k.across(y, 32 * b, 16 * s, col, quad);
+                x = multiply(y, faded[b], x);
+            }
+            state[s] = x;
+        }
+    }
+
+    // The same for a chunk with keys or values that are not finite, tick by tick: in a product of matrices they would reach
+    // ticks that they do not belong to, as zero times them is not zero.
+    template <bool READS>
+    static __device__ void advance_slowly(State &state, uint64_t begins, int n, float l2, const AttentionArgs &a, const Course &c,
+                                          int64_t q_at, int64_t k_at, int64_t v_at, int64_t out_at, int wave, int col, int quad)
+    {
+        const float e = __builtin_amdgcn_exp2f(l2);
+        const int d = 16 * wave + col;
+        for (int i = 0; i < n; ++i) {
+            const int64_t t = c.tick(i);
+            const bool begun = begins >> i & 1;
+            const float value = d < a.values ? element<TYPE>(a.v, v_at + t * a.vs.tick + d) * a.scale_added : 0.0f;
+            float sum = 0.0f;
+#pragma unroll
+            for (int s = 0; s < TILES; ++s) {
+                asm volatile("" ::: "memory");     // a few loads at a time: this path is to cost no registers
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int key = 16 * s + 4 * quad + r;
+                    float x = begun ? 0.0f : a.backward ? state[s][r] : state[s][r] * e;
+                    if (key < a.keys) {
+                        x = fmaf(element<TYPE>(a.k, k_at + t * a.ks.tick + key), value, x);
+                        if (READS) sum = fmaf(element<TYPE>(a.q, q_at + t * a.qs.tick + key), x, sum);
+                    }
+                    state[s][r] = a.backward ? x * e : x;
+                }
+            }
+            if constexpr (READS) {
+                sum += __shfl_xor(sum, 16);
+                sum += __shfl_xor(sum, 32);
+                if (a.out && quad == 0 && d < a.values)
+                    ((typename Element<TYPE>::one *)a.out)[out_at + t * a.os.tick + d] = (typename Element<TYPE>::one)(sum * a.scale_state);
+            }
+        }
+    }
+};
+
+// Workgroups are dealt to the eight XCDs in turn: each takes a run of neighbours, which share lines.
+__device__ __forceinline__ int64_t neighbour(int64_t id, int64_t all)
+{
+    const int64_t run = all / 8, rest = all % 8, x = id % 8;
+    return x * run + (x < rest ? x : rest) + id / 8;
+}
+
+// A workgroup has a row's head, or a segment of its ticks, and goes through the chunks with the state in registers; the
+// next chunk's rows are under way while it works on the present one.  CARRY: nothing is read, the states that the segments
+// would leave of nothing are.
+constexpr int attention_wavefronts(int d) { return 2; }   // of a SIMD
+
+template <int D, int TYPE, bool CARRY>
+__global__ __launch_bounds__(4 * D, attention_wavefronts(D)) void tabx_attention_kernel(const AttentionArgs a)
+{
+    typedef Attention<D, TYPE> A;
+    constexpr int C = A::C;
+    __shared__ typename A::In q, k, v;
+    __shared__ __bf16 within[A::MID][C * A::kWithin];
+    __shared__ int wild[2];                                    // of this chunk and the one before: not all is finite
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
     int turn = 0;
-    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, col = lane & 15, quad = lane >> 4;
-    for (int64_t w = blockIdx.x; w < a.works; w += gridDim.x) {
+    for (int64_t id = blockIdx.x; id < a.works; id += gridDim.x) {
+        const int64_t w = a.works <= gridDim.x ? neighbour(id, a.works) : id;
         const int segment = (int)(w % a.segments);
         const int64_t rh = w / a.segments, r = rh / a.heads;
         const int h = (int)(rh % a.heads);
         const int64_t first = segment * a.segment, last = min(first + a.segment, a.ticks);
         const int64_t env = r / a.units;
+        const int64_t q_at = r * a.qs.row + h * a.qs.head, k_at = r * a.ks.row + h * a.ks.head, v_at = r * a.vs.row + h * a.vs.head,
+                      out_at = r * a.os.row + h * a.os.head;
         if (a.controlled && a.controlled[r] == 0) {
             if (CARRY || !a.zero_out) continue;
             for (int64_t t = first; a.out && t < last; ++t)
-                for (int j = threadIdx.x; j < a.values; j += THREADS)
-                    put_element(a.out, t * a.os.tick + r * a.os.row + h * a.os.head + j, 0.0f, a.type);
+                for (int j = threadIdx.x; j < a.values; j += A::THREADS)
+                    ((typename Element<TYPE>::one *)a.out)[out_at + (a.backward ? a.ticks - 1 - t : t) * a.os.tick + j] = (typename Element<TYPE>::one)0.0f;
             if (a.state_out && segment == a.segments - 1)
-                for (int j = threadIdx.x; j < a.keys * a.values; j += THREADS)
+                for (int j = threadIdx.x; j < a.keys * a.values; j += A::THREADS)
                     a.state_out[rh * a.keys * a.values + (j / a.values) * a.state_key + (j % a.values) * a.state_value] = 0.0f;
             continue;
         }
-        const float l2 = log2_decay(a.log_decay, h);
-        f32x4 state[MINE][TILES];
+        const float l2 = fmaxf(log2_decay(a.log_decay, h), -1e9f);     // (all at once, and none of no ticks)
+        // a lane's elements of a state, as offsets that are worked out where they are needed and not kept meanwhile
+        const auto each = [&](int64_t along_keys, int64_t along_values, auto visit) {
+            int here = 0;
+            asm volatile("" : "+v"(here));
+            const int value = 16 * wave + col + here, first_key = 4 * quad + here;
 #pragma unroll
-        for (int m = 0; m < MINE; ++m)
-#pragma unroll
-            for (int n = 0; n < TILES; ++n)
+            for (int s = 0; s < A::TILES; ++s)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int key = 16 * n + 4 * quad + i, value = 16 * (wave * MINE + m) + col;
-                    float s = 0.0f;
-                    if (!CARRY && key < a.keys && value < a.values) {
-                        if (a.carried) s = a.carried[(w * a.keys + key) * a.values + value];
-                        else if (a.state_in) s = a.state_in[rh * a.keys * a.values + key * a.state_key + value * a.state_value];
-                    }
-                    state[m][n][i] = s;
+                    const int key = first_key + 16 * s + i;
+                    if (key < a.keys && value < a.values) visit(s, i, key * (int)along_keys + value * (int)along_values);
                 }
+        };
+        typename A::State state;
+#pragma unroll
+        for (int s = 0; s < A::TILES; ++s) state[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (!CARRY && a.carried) {
+            const float *const from = a.carried + w * a.keys * a.values;
+            each(a.values, 1, [&](int s, int i, int at) { state[s][i] = from[at]; });
+        } else if (!CARRY && a.state_in) {
+            const float *const from = a.state_in + rh * a.keys * a.values;
+            each(a.state_key, a.state_value, [&](int s, int i, int at) { state[s][i] = from[at]; });
+        }
         float kept = 1.0f;
+        typename A::Rows qr, kr, vr;
+        int flag = 0;
+        Course next = {a.ticks, first, a.backward};
+        const auto fetch = [&](int n) {
+            if constexpr (!CARRY) A::load(qr, a.q, q_at, a.qs.tick, next, n, a.keys);
+            A::load(kr, a.k, k_at, a.ks.tick, next, n, a.keys);
+            A::load(vr, a.v, v_at, a.vs.tick, next, n, a.values);
+            flag = 0;
+            if (a.fresh && lane < n) {
+                // backwards, an episode begins behind the tick where, forwards, the next one does
+                const int64_t t = next.begin + lane;
+                if (!a.backward) flag = a.fresh[t * a.envs + env];
+                else if (t > 0) flag = a.fresh[(a.ticks - t) * a.envs + env];
+            }
+        };
+        if (first < last) fetch((int)min((int64_t)C, last - first));
         for (int64_t begin = first; begin < last; begin += C) {
             const int n = (int)min((int64_t)C, last - begin);
-            // bit i: an episode begins with the chunk's tick i
-            const int64_t mine = begin + (lane < n ? lane : 0);
-            const int64_t flag = a.backward ? a.ticks - mine : mine;
-            const bool here = a.fresh && lane < n && !(a.backward && mine == 0) && a.fresh[flag * a.envs + env] != 0;
-            const uint64_t begins = __ballot(here);
-            const int newest = begins ? 63 - __builtin_clzll(begins) : 0;      // the last episode's first tick
+            const Course here = next;
             turn ^= 1;
             if (threadIdx.x == 0) wild[turn] = 0;
-            __syncthreads();                                   // the chunk before has been read
-            for (int at = threadIdx.x; at < C * D; at += THREADS) {
-                const int i = at / D, d = at % D;
-                const int64_t t = a.backward ? a.ticks - 1 - (begin + i) : begin + i;
-                const bool key = i < n && d < a.keys, value = i < n && d < a.values;
-                if (!CARRY) qs[i][d] = key ? element_of(a.q, t * a.qs.tick + r * a.qs.row + h * a.qs.head + d, a.type) : 0.0f;
-                const float kv = key ? element_of(a.k, t * a.ks.tick + r * a.ks.row + h * a.ks.head + d, a.type) : 0.0f;
-                if (!CARRY) ks[i][d] = kv;
-                kt[d][i] = i >= newest ? kv : 0.0f;
-                float vv = value ? element_of(a.v, t * a.vs.tick + r * a.vs.row + h * a.vs.head + d, a.type) : 0.0f;
-                if (!(fabsf(vv) < INFINITY)) {
-                    atomicOr(&wild[turn], 1u << i);
-                    vv = 0.0f;
-                }
-                vt[d][i] = vv;
-            }
+            __syncthreads();                                   // the chunk before has been worked on
+            if constexpr (!CARRY) A::store(q, qr);
+            const uint32_t odd = A::store(k, kr) | A::store(v, vr);
+            if (__ballot(odd != 0) && lane == 0) wild[turn] = 1;
+            const uint64_t begins = __ballot(flag != 0);       // bit i: an episode begins with the chunk's tick i
+            next.begin += C;
+            if (next.begin < last) fetch((int)min((int64_t)C, last - next.begin));
             __syncthreads();
             if constexpr (!CARRY) {
-                // the products of queries and keys, tiles of 16 x 16 on and below the diagonal
-                for (int tile = wave; tile < (C / 16) * (C / 16 + 1) / 2; tile += WAVES) {
-                    const int I = tile == 0 ? 0 : 1, J = tile == 2 ? 1 : 0;
-                    f32x4 p = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int s = 0; s < TILES; ++s) {
-                        const f32x4 x = *(const f32x4 *)&qs[16 * I + col][16 * s + 4 * quad], y = *(const f32x4 *)&ks[16 * J + col][16 * s + 4 * quad];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) p = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[i], p, 0, 0, 0);
-                    }
-                    const int j = 16 * J + col;
-#pragma unroll
-                    for (int s = 0; s < 4; ++s) {
-                        const int i = 16 * I + 4 * quad + s;
-                        const uint64_t up = begins & ((2ull << i) - 1);            // begun up to i
-                        const bool same = j <= i && (up >> j) <= 1;                // none of them behind j
-                        within[i][j] = same ? p[s] * decayed(l2, i - j) : 0.0f;
-                    }
-                }
+                A::compare(within, q, k, begins, l2, a.scale_within, wave, col, quad);
                 __syncthreads();
             }
-            const uint32_t odd = wild[turn];
-#pragma unroll
-            for (int m = 0; m < MINE; ++m) {
-                const int value = 16 * (wave * MINE + m) + col;
-                if constexpr (!CARRY) {
-#pragma unroll
-                    for (int I = 0; I < C / 16; ++I) {
-                        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                        for (int s = 0; s < TILES; ++s) {
-                            const f32x4 x = *(const f32x4 *)&qs[16 * I + col][16 * s + 4 * quad];
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) o = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], state[m][s][i], o, 0, 0, 0);
-                        }
-#pragma unroll
-                        for (int s = 0; s < 4; ++s) {
-                            const int i = 16 * I + 4 * quad + s;
-                            o[s] = begins & ((2ull << i) - 1) ? 0.0f : o[s] * (decayed(l2, i + 1 - a.backward) * a.scale_state);
-                        }
-                        f32x4 p = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                        for (int J = 0; J <= I; ++J) {
-                            const f32x4 x = *(const f32x4 *)&within[16 * I + col][16 * J + 4 * quad], y = *(const f32x4 *)&vt[value][16 * J + 4 * quad];
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) p = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[i], p, 0, 0, 0);
-                        }
-#pragma unroll
-                        for (int s = 0; s < 4; ++s) {
-                            const int i = 16 * I + 4 * quad + s;
-                            float within_sum = p[s];
-                            // values that are not finite, of ticks that count here (zero times them would not be zero)
-                            if (odd && i < n && value < a.values) {
-                                for (uint32_t left = odd; left; left &= left - 1) {
-                                    const int j = __builtin_ctz(left);
-                                    const int64_t t = a.backward ? a.ticks - 1 - (begin + j) : begin + j;
-                                    const float x = element_of(a.v, t * a.vs.tick + r * a.vs.row + h * a.vs.head + value, a.type);
-                                    const bool same = j <= i && ((begins & ((2ull << i) - 1)) >> j) <= 1;
-                                    if (same && !(fabsf(x) < INFINITY)) within_sum += within[i][j] * x;
-                                }
-                            }
-                            if (a.out && i < n && value < a.values) {
-                                const int64_t t = a.backward ? a.ticks - 1 - (begin + i) : begin + i;
-                                put_element(a.out, t * a.os.tick + r * a.os.row + h * a.os.head + value, fmaf(within_sum, a.scale_within, o[s]), a.type);
-                            }
-                        }
-                    }
-                }
-                // the state behind the chunk
-                const float left = decayed(l2, n);
-                f32x4 fading[C / 16];                          // this lane's values, faded by the ticks behind theirs
-#pragma unroll
-                for (int J = 0; J < C / 16; ++J) {
-                    fading[J] = *(const f32x4 *)&vt[value][16 * J + 4 * quad];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) fading[J][i] *= decayed(l2, n - 1 - (16 * J + 4 * quad + i) + a.backward) * a.scale_added;
-                }
-#pragma unroll
-                for (int s = 0; s < TILES; ++s) {
-                    f32x4 &x = state[m][s];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) x[i] = begins ? 0.0f : x[i] * left;
-#pragma unroll
-                    for (int J = 0; J < C / 16; ++J) {
-                        const f32x4 y = *(const f32x4 *)&kt[16 * s + col][16 * J + 4 * quad];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) x = __builtin_amdgcn_mfma_f32_16x16x4f32(y[i], fading[J][i], x, 0, 0, 0);
-                    }
-                    if (odd && value < a.values) {
-                        for (uint32_t rest = odd; rest; rest &= rest - 1) {
-                            const int j = __builtin_ctz(rest);
-                            if (j < newest) continue;
-                            const int64_t t = a.backward ? a.ticks - 1 - (begin + j) : begin + j;
-                            const float y = element_of(a.v, t * a.vs.tick + r * a.vs.row + h * a.vs.head + value, a.type);
-                            if (!(fabsf(y) < INFINITY))
-#pragma unroll
-                                for (int i = 0; i < 4; ++i)
-                                    x[i] += kt[16 * s + 4 * quad + i][j] * (y * (decayed(l2, n - 1 - j + a.backward) * a.scale_added));
-                        }
-                    }
-                }
-            }
-            kept = begins || kept < 0.0f ? -1.0f : kept * decayed(l2, n);
+            if (__builtin_expect(wild[turn], 0)) A::template advance_slowly<!CARRY>(state, begins, n, l2, a, here, q_at, k_at, v_at, out_at, wave, col, quad);
+            else A::template advance<!CARRY>(state, within, q, k, v, begins, n, l2, a, here, out_at, wave, col, quad);
+            kept = begins || kept < 0.0f ? -1.0f : kept * __builtin_amdgcn_exp2f(l2 * (float)n);
         }
         float *const to = CARRY ? a.carried + w * a.keys * a.values : segment == a.segments - 1 ? a.state_out : nullptr;
         if (CARRY && threadIdx.x == 0) a.kept[w] = kept;
         if (!to) continue;
         // backwards, what is left for the state before the first tick, if that belongs to its episode
         const bool cut = !CARRY && a.backward && a.fresh && a.ticks > 0 && a.fresh[env] != 0;
-#pragma unroll
-        for (int m = 0; m < MINE; ++m)
-#pragma unroll
-            for (int n = 0; n < TILES; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int key = 16 * n + 4 * quad + i, value = 16 * (wave * MINE + m) + col;
-                    if (key >= a.keys || value >= a.values) continue;
-                    if (CARRY) to[key * a.values + value] = state[m][n][i];
-                    else to[rh * a.keys * a.values + key * a.state_key + value * a.state_value] = cut ? 0.0f : state[m][n][i];
-                }
+        if (CARRY) {
+            each(a.values, 1, [&](int s, int i, int at) { to[at] = state[s][i]; });
+        } else {
+            float *const of = to + rh * a.keys * a.values;
+            each(a.state_key, a.state_value, [&](int s, int i, int at) { of[at] = cut ? 0.0f : state[s][i]; });
+        }
     }
 }
 

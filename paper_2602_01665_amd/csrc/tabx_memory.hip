@@ -204,20 +204,22 @@ static int64_t attention_workspace(int64_t ticks, int64_t rows, int32_t heads, i
     return s.count == 1 ? 0 : rows * heads * s.count * ((int64_t)keys * values + 1) * (int64_t)sizeof(float);
 }
 
-template <int D, bool CARRY>
+template <bool CARRY, int D>
 static int launch_attention(const AttentionArgs &a, void *stream)
 {
-    return launch(tabx_attention_kernel<D, CARRY>, least(a.works, kMostGroups), D >= 64 ? 256 : 4 * D, a, stream);
+    return launch(a.type == TABX_F32    ? tabx_attention_kernel<D, TABX_F32, CARRY>
+                  : a.type == TABX_BF16 ? tabx_attention_kernel<D, TABX_BF16, CARRY>
+                                        : tabx_attention_kernel<D, TABX_F16, CARRY>,
+                  least(a.works, kMostGroups), 4 * D, a, stream);
 }
 
 template <bool CARRY>
 static int attention_of_width(const AttentionArgs &a, void *stream)
 {
     const int width = a.keys > a.values ? a.keys : a.values;
-    if (width <= 16) return launch_attention<16, CARRY>(a, stream);
-    if (width <= 32) return launch_attention<32, CARRY>(a, stream);
-    if (width <= 64) return launch_attention<64, CARRY>(a, stream);
-    return launch_attention<128, CARRY>(a, stream);
+    if (width <= 32) return launch_attention<CARRY, 32>(a, stream);
+    if (width <= 64) return launch_attention<CARRY, 64>(a, stream);
+    return launch_attention<CARRY, 128>(a, stream);
 }
 
 static int attention(AttentionArgs a, void *workspace, void *stream)
