@@ -56,21 +56,8 @@ __device__ __forceinline__ float element(const void *data, int64_t at)
     return (float)((const typename Element<TYPE>::one *)data)[at];
 }
 
-__device__ __forceinline__ float element_of(const void *data, int64_t at, int type)
-{
-    return type == TABX_F32 ? element<TABX_F32>(data, at) : type == TABX_BF16 ? element<TABX_BF16>(data, at) : element<TABX_F16>(data, at);
-}
-
-__device__ __forceinline__ void put_element(void *data, int64_t at, float v, int type)
-{
-    if (type == TABX_F32) ((float *)data)[at] = v;
-    else if (type == TABX_BF16) ((__bf16 *)data)[at] = (__bf16)v;
-    else ((_Float16 *)data)[at] = (_Float16)v;
-}
-
 // --- one tick -----------------------------------------------------------------------------------
 
-// A wavefront has a row's head: its lanes lie along the values, and there are several of the state's lines at a time.
 struct StepArgs {
     const void *q, *k, *v;
     void       *out;
@@ -79,35 +66,80 @@ struct StepArgs {
     const uint8_t *fresh, *controlled;
     float      *state;
     int64_t     works;             // rows x heads
-    int32_t     heads, units, keys, values, type;
+    int32_t     heads, units, keys, values;
     float       scale;
 };
 
-template <int LANES>
+// A state is a run of keys x values floats.  LANES lanes have a row's head (64: a whole wavefront); lane l has four
+// consecutive values of every (4 LANES / VALUES)-th line of the state, so that the lanes read and write 16 bytes each of
+// one run.  VALUES: the values rounded up to a power of two; lanes beyond the last value idle.
+template <int TYPE, int VALUES, int LANES>
 __global__ __launch_bounds__(256) void tabx_attention_step_kernel(const StepArgs a)
 {
-    constexpr int LINES = 64 / LANES;
-    const int lane = (int)threadIdx.x & 63, d = lane % LANES, line = lane / LANES;
-    for (int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); w < a.works; w += (int64_t)gridDim.x * 4) {
-        const int64_t r = w / a.heads;
-        const int h = (int)(w % a.heads);
+    typedef typename Element<TYPE>::one T;
+    typedef f32x4 Anywhere __attribute__((aligned(4)));
+    constexpr int ACROSS = VALUES / 4, LINES = LANES / ACROSS, WORKS = 256 / LANES, AT_ONCE = 8;
+    const int lane = (int)threadIdx.x % LANES, d = 4 * (lane % ACROSS), line = lane / ACROSS;
+    for (int64_t w = (int64_t)blockIdx.x * WORKS + threadIdx.x / LANES; w < a.works; w += (int64_t)gridDim.x * WORKS) {
+        const int64_t r = (uint32_t)w / (uint32_t)a.heads;     // (rows x heads has 31 bits)
+        const int h = (int)((uint32_t)w % (uint32_t)a.heads);
         if (a.controlled && a.controlled[r] == 0) continue;
-        const bool forget = a.fresh && a.fresh[r / a.units] != 0;
+        const bool forget = a.fresh && a.fresh[(uint32_t)r / (uint32_t)a.units] != 0;
         const float e = decayed(log2_decay(a.log_decay, h), 1);
-        float *state = a.state + w * a.keys * a.values;
-        const int64_t q = r * a.qs.row + h * a.qs.head, k = r * a.ks.row + h * a.ks.head, v = r * a.vs.row + h * a.vs.head;
-        for (int j = d; j < a.values; j += LANES) {
-            const float value = element_of(a.v, v + j, a.type);
-            float sum = 0.0f;
-            for (int i = line; i < a.keys; i += LINES) {
-                float s = state[(int64_t)i * a.values + j];
-                s = fmaf(element_of(a.k, k + i, a.type), value, forget ? 0.0f : e * s);
-                state[(int64_t)i * a.values + j] = s;
-                sum = fmaf(element_of(a.q, q + i, a.type), s, sum);
-            }
+        const int count = a.values - d;            // of this lane's four values
+        const T *const q = (const T *)a.q + r * a.qs.row + h * a.qs.head, *const k = (const T *)a.k + r * a.ks.row + h * a.ks.head,
+                *const v = (const T *)a.v + r * a.vs.row + h * a.vs.head + d;
+        float *const state = a.state + w * a.keys * a.values + d;
+        f32x4 value = {0.0f, 0.0f, 0.0f, 0.0f}, sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int n = LANES; n < 64; n *= 2) sum += __shfl_xor(sum, n);
-            if (line == 0) put_element(a.out, r * a.os.row + h * a.os.head + j, sum * a.scale, a.type);
+        for (int n = 0; n < 4; ++n)
+            if (n < count) value[n] = (float)v[n];
+        if (a.values % 4 == 0) {
+            for (int i = line; i < a.keys; i += LINES * AT_ONCE) {
+                f32x4 s[AT_ONCE];
+                float x[AT_ONCE], y[AT_ONCE];
+#pragma unroll
+                for (int n = 0; n < AT_ONCE; ++n) {
+                    const int key = min(i + n * LINES, a.keys - 1);
+                    if (count > 0) s[n] = *(const Anywhere *)(state + key * a.values);
+                    x[n] = (float)k[key], y[n] = (float)q[key];
+                }
+#pragma unroll
+                for (int n = 0; n < AT_ONCE; ++n) {
+                    if (i + n * LINES >= a.keys || count <= 0) continue;
+                    const f32x4 old = forget ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : s[n] * e;
+                    const f32x4 now = {fmaf(x[n], value.x, old.x), fmaf(x[n], value.y, old.y), fmaf(x[n], value.z, old.z), fmaf(x[n], value.w, old.w)};
+                    *(Anywhere *)(state + (i + n * LINES) * a.values) = now;
+                    sum = f32x4{fmaf(y[n], now.x, sum.x), fmaf(y[n], now.y, sum.y), fmaf(y[n], now.z, sum.z), fmaf(y[n], now.w, sum.w)};
+                }
+            }
+        } else {
+            for (int i = line; i < a.keys; i += LINES) {
+                const float x = (float)k[i], y = (float)q[i];
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    if (n >= count) continue;
+                    float s = state[i * a.values + n];
+                    s = fmaf(x, value[n], forget ? 0.0f : e * s);
+                    state[i * a.values + n] = s;
+                    sum[n] = fmaf(y, s, sum[n]);
+                }
+            }
+        }
+#pragma unroll
+        for (int n = ACROSS; n < LANES; n *= 2)
+#pragma unroll
+            for (int m = 0; m < 4; ++m) sum[m] += __shfl_xor(sum[m], n);
+        if (line == 0 && count > 0) {
+            T *const out = (T *)a.out + r * a.os.row + h * a.os.head + d;
+            sum *= a.scale;
+            if (count >= 4) {
+                store_four<TYPE>(out, sum);
+            } else {
+#pragma unroll
+                for (int n = 0; n < 3; ++n)
+                    if (n < count) out[n] = (T)sum[n];
+            }
         }
     }
 }

@@ -158,14 +158,21 @@ static Strides strides_of(const TabxHeads &m) { return Strides{m.tick_stride, m.
 
 // --- rotation -----------------------------------------------------------------------------------
 
-template <int LANES>
+template <int TYPE, bool INTERLEAVED, int LANES>
 static int launch_rotary(const RotaryArgs &a, void *stream)
 {
-    const int64_t groups = least(quotient_up(a.rows, 256 / LANES), kMostGroups);
-    return launch(a.type == TABX_F32    ? tabx_rotary_kernel<LANES, TABX_F32>
-                  : a.type == TABX_BF16 ? tabx_rotary_kernel<LANES, TABX_BF16>
-                                        : tabx_rotary_kernel<LANES, TABX_F16>,
-                  groups, 256, a, stream);
+    return launch(tabx_rotary_kernel<LANES, TYPE, INTERLEAVED>, least(quotient_up(a.rows, 256 / LANES), kMostGroups), 256, a, stream);
+}
+
+template <int TYPE, bool INTERLEAVED>
+static int rotary(const RotaryArgs &a, void *stream)
+{
+    const int lanes = (a.pairs + 3) / 4;
+    if (lanes <= 4) return launch_rotary<TYPE, INTERLEAVED, 4>(a, stream);
+    if (lanes <= 8) return launch_rotary<TYPE, INTERLEAVED, 8>(a, stream);
+    if (lanes <= 16) return launch_rotary<TYPE, INTERLEAVED, 16>(a, stream);
+    if (lanes <= 32) return launch_rotary<TYPE, INTERLEAVED, 32>(a, stream);
+    return launch_rotary<TYPE, INTERLEAVED, 64>(a, stream);
 }
 
 // --- linear attention ---------------------------------------------------------------------------
@@ -238,6 +245,24 @@ static int attention(AttentionArgs a, void *workspace, void *stream)
         if ((rc = launch(tabx_attention_join_kernel, least(quotient_up(states, 256), kMostGroups), 256, a, stream))) return rc;
     }
     return attention_of_width<false>(a, stream);
+}
+
+template <int TYPE, int VALUES, int LANES>
+static int launch_step(const StepArgs &a, void *stream)
+{
+    return launch(tabx_attention_step_kernel<TYPE, VALUES, LANES>, least(quotient_up(a.works, 256 / LANES), kMostGroups), 256, a, stream);
+}
+
+// States of few elements share a wavefront.
+template <int TYPE>
+static int attention_step(const StepArgs &a, void *stream)
+{
+    if (a.values <= 4) return a.keys <= 16 ? launch_step<TYPE, 4, 8>(a, stream) : launch_step<TYPE, 4, 64>(a, stream);
+    if (a.values <= 8) return a.keys <= 16 ? launch_step<TYPE, 8, 16>(a, stream) : launch_step<TYPE, 8, 64>(a, stream);
+    if (a.values <= 16) return a.keys <= 32 ? launch_step<TYPE, 16, 16>(a, stream) : launch_step<TYPE, 16, 64>(a, stream);
+    if (a.values <= 32) return launch_step<TYPE, 32, 64>(a, stream);
+    if (a.values <= 64) return launch_step<TYPE, 64, 64>(a, stream);
+    return launch_step<TYPE, 128, 64>(a, stream);
 }
 
 static int check_workspace(const void *workspace, int64_t bytes, int64_t needed)
@@ -354,15 +379,12 @@ int tabx_rotary(int64_t rows, int32_t heads, int32_t width, const TabxHeads *x, 
     a.y = y->data, a.y_row = y->row_stride, a.y_head = y->head_stride;
     a.row_mask = row_mask;
     a.frequency = frequency;
-    a.rows = rows, a.heads = heads, a.width = width, a.type = x->type;
-    a.num_axes = num_axes, a.interleaved = interleaved != 0, a.sign = inverse ? -1.0 : 1.0;
+    a.rows = rows, a.heads = heads, a.width = width;
+    a.num_axes = num_axes, a.sign = inverse ? -1.0 : 1.0;
     a.copies = x->data != y->data;
-    const int lanes = (a.pairs + 3) / 4;
-    if (lanes <= 4) return launch_rotary<4>(a, stream);
-    if (lanes <= 8) return launch_rotary<8>(a, stream);
-    if (lanes <= 16) return launch_rotary<16>(a, stream);
-    if (lanes <= 32) return launch_rotary<32>(a, stream);
-    return launch_rotary<64>(a, stream);
+    if (x->type == TABX_F32) return interleaved ? rotary<TABX_F32, true>(a, stream) : rotary<TABX_F32, false>(a, stream);
+    if (x->type == TABX_BF16) return interleaved ? rotary<TABX_BF16, true>(a, stream) : rotary<TABX_BF16, false>(a, stream);
+    return interleaved ? rotary<TABX_F16, true>(a, stream) : rotary<TABX_F16, false>(a, stream);
 }
 
 int tabx_linear_attention_step(int64_t rows, int32_t heads, int32_t key_width, int32_t value_width, const TabxHeads *q,
@@ -382,11 +404,8 @@ int tabx_linear_attention_step(int64_t rows, int32_t heads, int32_t key_width, i
     a.log_decay = log_decay, a.fresh = fresh, a.controlled = controlled;
     a.state = state;
     a.works = rows * heads, a.heads = heads, a.units = units, a.keys = key_width, a.values = value_width;
-    a.type = q->type, a.scale = scale;
-    const int64_t groups = least(quotient_up(a.works, 4), kMostGroups);
-    if (value_width <= 16) return launch(tabx_attention_step_kernel<16>, groups, 256, a, stream);
-    if (value_width <= 32) return launch(tabx_attention_step_kernel<32>, groups, 256, a, stream);
-    return launch(tabx_attention_step_kernel<64>, groups, 256, a, stream);
+    a.scale = scale;
+    return q->type == TABX_F32 ? attention_step<TABX_F32>(a, stream) : q->type == TABX_BF16 ? attention_step<TABX_BF16>(a, stream) : attention_step<TABX_F16>(a, stream);
 }
 
 int64_t tabx_linear_attention_workspace(int64_t ticks, int64_t rows, int32_t heads, int32_t key_width, int32_t value_width)

@@ -123,22 +123,27 @@ __global__ __launch_bounds__(threads_of(LANES)) void tabx_rms_kernel(const RmsAr
         for (int q = 0; q < PIECES - 1; ++q) squares = fma4(v[q], v[q], squares);
         const float rstd = rsqrtf(fmaf(row_sum<LANES>(sum_of(squares), slots[turn]), a.inv_width, a.eps));
         if (a.rstd && cut.lane == 0) a.rstd[h.at] = rstd;
-#pragma unroll
-        for (int q = 0; q < PIECES; ++q) v[q] = v[q] * rstd * w[q];
         if (a.y_type == TABX_E4M3) {
-            // (elements that lie in two pieces are as large in both)
+            // y / scale is (s w) (448 / largest |s w|): rstd is in both and need not be rounded into either.  (Elements that
+            // lie in two pieces are as large in both.)
             float most = 0.0f;
 #pragma unroll
-            for (int q = 0; q < PIECES; ++q)
+            for (int q = 0; q < PIECES; ++q) {
+                v[q] *= w[q];
                 most = fmaxf(most, fmaxf(fmaxf(fabsf(v[q].x), fabsf(v[q].y)), fmaxf(fabsf(v[q].z), fabsf(v[q].w))));
-            const float scale = fmaxf(row_max<LANES>(most, slots[turn + 1]) / kLargestE4m3, kLeastScale);
+            }
+            most = row_max<LANES>(most, slots[turn + 1]);
+            const float scale = fmaxf(most * rstd / kLargestE4m3, kLeastScale);        // (the least where an infinite sum made rstd 0)
             if (cut.lane == 0) a.scale[h.at] = scale;
-            const float inverse = 1.0f / scale;
+            const bool small = !(scale > kLeastScale && most > 1e-30f);                // 448 / most might be infinite
+            const float one = small ? rstd : kLargestE4m3 / most, other = small ? 1.0f / scale : 1.0f;
 #pragma unroll
-            for (int q = 0; q < PIECES; ++q) v[q] *= inverse;
+            for (int q = 0; q < PIECES; ++q) v[q] = v[q] * one * other;
             if (a.stream) store_row_e4m3<true>(v, a.y, h.at * a.y_stride, cut, a.width);
             else store_row_e4m3<false>(v, a.y, h.at * a.y_stride, cut, a.width);
         } else {
+#pragma unroll
+            for (int q = 0; q < PIECES; ++q) v[q] = v[q] * rstd * w[q];
             if (a.stream) store_row<true>(v, a.y, a.y_type, h.at * a.y_stride, cut, a.width);
             else store_row(v, a.y, a.y_type, h.at * a.y_stride, cut, a.width);
         }
