@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
@@ -28,10 +29,18 @@ HIPCC_FLAGS = [
 
 def build(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc] + HIPCC_FLAGS + SOURCES + LEARNER_SOURCES + MEMORY_SOURCES + ["-o", LIB_PATH]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+    with tempfile.TemporaryDirectory() as tmp:     # the sources side by side, then one library of their objects
+        running = []
+        for source in SOURCES + LEARNER_SOURCES + MEMORY_SOURCES:
+            to = os.path.join(tmp, os.path.basename(source) + ".o")
+            cmd = [hipcc] + [f for f in HIPCC_FLAGS if f != "-shared"] + ["-c", source, "-o", to]
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            running.append((cmd, to, subprocess.Popen(cmd)))
+        failed = [cmd for cmd, _, p in running if p.wait() != 0]
+        if failed:
+            raise subprocess.CalledProcessError(1, failed[0])
+        subprocess.run([hipcc] + HIPCC_FLAGS + [to for _, to, _ in running] + ["-o", LIB_PATH], check=True)
     return LIB_PATH
 
 

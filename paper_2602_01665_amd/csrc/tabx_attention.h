@@ -160,7 +160,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int chunk_of(int type) { return type == TABX_BF16 ? 64 : 32; }
+constexpr int chunk_of(int d, int type) { return type == TABX_BF16 && d > 32 ? 64 : 32; }
 
 template <int N>
 __device__ __forceinline__ void split(bf16x4 (&part)[N], f32x4 v)
@@ -188,28 +188,35 @@ __device__ __forceinline__ f32x4 multiply(const bf16x8 (&a)[NA], const bf16x8 (&
 }
 
 // Eight elements of a row as they lie in memory.
-template <int TYPE> struct Eight { u32x4 v[TYPE == TABX_F32 ? 2 : 1]; };
-
 template <int TYPE>
-__device__ __forceinline__ void load_eight(Eight<TYPE> &e, const void *data, int64_t at, int count)
-{
+struct Eight {
     typedef typename Element<TYPE>::one T;
     typedef u32x4 Anywhere __attribute__((aligned(2)));
-    const T *from = (const T *)data + at;
+    static constexpr int PIECES = TYPE == TABX_F32 ? 2 : 1;
+    u32x4 v[PIECES];
+
+    __device__ __forceinline__ void load(const T *from)
+    {
 #pragma unroll
-    for (int n = 0; n < (TYPE == TABX_F32 ? 2 : 1); ++n) e.v[n] = u32x4{0, 0, 0, 0};
-    if (count >= 8) {
+        for (int n = 0; n < PIECES; ++n) v[n] = ((const Anywhere *)from)[n];
+    }
+    // Those below `count`, and zeros.
+    __device__ __forceinline__ void load_some(const T *from, int count)
+    {
 #pragma unroll
-        for (int n = 0; n < (TYPE == TABX_F32 ? 2 : 1); ++n) e.v[n] = ((const Anywhere *)from)[n];
-    } else if (count > 0) {                        // a width that is no multiple of eight
+        for (int n = 0; n < PIECES; ++n) v[n] = u32x4{0, 0, 0, 0};
+        if (count >= 8) {
+            load(from);
+        } else if (count > 0) {                    // a width that is no multiple of eight
 #pragma unroll
-        for (int i = 0; i < 7; ++i) {
-            if (i >= count) continue;
-            if constexpr (TYPE == TABX_F32) e.v[i / 4][i % 4] = ((const uint32_t *)from)[i];
-            else e.v[0][i / 2] |= (uint32_t)((const uint16_t *)from)[i] << 16 * (i % 2);
+            for (int i = 0; i < 7; ++i) {
+                if (i >= count) continue;
+                if constexpr (TYPE == TABX_F32) v[i / 4][i % 4] = ((const uint32_t *)from)[i];
+                else v[0][i / 2] |= (uint32_t)((const uint16_t *)from)[i] << 16 * (i % 2);
+            }
         }
     }
-}
+};
 
 // Not 0 in a bit of its own if one of them is not finite (an exponent of ones carries).
 template <int TYPE>
@@ -291,7 +298,7 @@ struct Course {
 
 template <int D, int TYPE>
 struct Attention {
-    static constexpr int C = chunk_of(TYPE), IN = Parts<TYPE>::in, MID = Parts<TYPE>::mid;
+    static constexpr int C = chunk_of(D, TYPE), IN = Parts<TYPE>::in, MID = Parts<TYPE>::mid;
     static constexpr int WAVES = D / 16, THREADS = 64 * WAVES, PASSES = C * D / 8 / THREADS, TILES = D / 16;
     typedef Tile<D, C, IN> In;
     static constexpr int kWithin = C + 8;          // distance of rows of the products of queries and keys
@@ -305,11 +312,18 @@ struct Attention {
     static __device__ __forceinline__ void load(Rows &rows, const void *data, int64_t at, int64_t tick, const Course &c, int n, int width)
     {
         constexpr int across = D / 8;
-        const int d = 8 * ((int)threadIdx.x % across);
+        const int d = 8 * ((int)threadIdx.x % across), row = (int)threadIdx.x / across;
+        const int64_t step = c.backward ? -tick : tick;
+        const typename Element<TYPE>::one *const from = (const typename Element<TYPE>::one *)data + at + c.tick(0) * tick + row * step + d;
+        if (n == C && width == D) {                // (the same for all: no lane has to be asked)
 #pragma unroll
-        for (int p = 0; p < PASSES; ++p) {
-            const int i = p * (THREADS / across) + (int)threadIdx.x / across;
-            load_eight<TYPE>(rows.e[p], data, at + c.tick(i < n ? i : 0) * tick + d, i < n ? width - d : 0);
+            for (int p = 0; p < PASSES; ++p) rows.e[p].load(from + p * (THREADS / across) * step);
+        } else {
+#pragma unroll
+            for (int p = 0; p < PASSES; ++p) {
+                const int i = p * (THREADS / across) + row;
+                rows.e[p].load_some(from + p * (THREADS / across) * step, i < n ? width - d : 0);
+            }
         }
     }
     static __device__ __forceinline__ uint32_t store(In &tile, const Rows &rows)
@@ -328,7 +342,7 @@ struct Attention {
     // tiles of 16 x 16 on and below the diagonal, dealt to the wavefronts.  Rows are queries; along them the keys lie in the
     // order of `along_results`, so that a lane's eight are next to each other.
     static __device__ __forceinline__ void compare(__bf16 (&within)[MID][C * kWithin], const In &q, const In &k, uint64_t begins, float l2,
-                                                   float scale, int wave, int col, int quad)
+                                                   const float (&power)[4], float scale, int wave, int col, int quad)
     {
         constexpr int tiles = C / 16 * (C / 16 + 1) / 2;
         for (int tile = wave; tile < tiles; tile += WAVES) {
@@ -341,13 +355,20 @@ struct Attention {
                 q.along(y, 16 * I, 32 * s, col, quad);
                 p = multiply(x, y, p);
             }
-            const int i = 16 * I + col;
-            const uint64_t up = begins & ((2ull << i) - 1);            // episodes begun up to the query's tick
+            const int i = 16 * I + col, first = 16 * J + 4 * quad;
+            if (I > J) {
+                const float fade = __builtin_amdgcn_exp2f(l2 * (float)(i - first - 3)) * scale;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int j = 16 * J + 4 * quad + r;
-                const bool same = j <= i && (up >> j) <= 1;            // none of them behind the key's
-                p[r] = same ? p[r] * (__builtin_amdgcn_exp2f(l2 * (float)(i - j)) * scale) : 0.0f;
+                for (int r = 0; r < 4; ++r) p[r] *= fade * power[3 - r];
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) p[r] = first + r <= i ? p[r] * (__builtin_amdgcn_exp2f(l2 * (float)(i - first - r)) * scale) : 0.0f;
+            }
+            if (begins) {                          // (the same for all)
+                const uint64_t up = begins & ((2ull << i) - 1);        // episodes begun up to the query's tick
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (first + r <= i && (up >> (first + r)) > 1) p[r] = 0.0f;        // one of them behind the key's
             }
             bf16x4 part[MID];
             split(part, p);
@@ -363,8 +384,8 @@ struct Attention {
     // What a chunk's queries read, and the state behind the chunk.
     template <bool READS>
     static __device__ __forceinline__ void advance(State &state, const __bf16 (&within)[MID][C * kWithin], const In &q, const In &k, const In &v,
-                                                   uint64_t begins, int n, float l2, const AttentionArgs &a, const Course &c, int64_t out_at,
-                                                   int wave, int col, int quad)
+                                                   uint64_t begins, int n, float l2, const float (&power)[4], const AttentionArgs &a,
+                                                   const Course &c, int64_t out_at, int wave, int col, int quad)
     {
         bf16x8 values[C / 32][IN];                 // this lane's: 8 ticks of its column, of every 32
 #pragma unroll
@@ -379,9 +400,13 @@ struct Attention {
 #pragma unroll
                 for (int m = 0; m < MID; ++m) held[s][m] = join(x[m], y[m]);
             }
+            const int d = 16 * wave + 4 * quad;
+            const int64_t step = c.backward ? -a.os.tick : a.os.tick;
+            typename Element<TYPE>::one *const out = (typename Element<TYPE>::one *)a.out + out_at + c.tick(0) * a.os.tick + col * step + d;
 #pragma unroll
             for (int I = 0; I < C / 16; ++I) {
                 if (16 * I >= n) break;
+                __builtin_amdgcn_sched_barrier(0); // (operands of all of them at a time would not fit)
                 const int i = 16 * I + col;
                 f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -391,9 +416,12 @@ struct Attention {
                     o = multiply(held[s], x, o);
                 }
                 const float fade = __builtin_amdgcn_exp2f(l2 * (float)(i + 1 - a.backward)) * a.scale_state;
-                const bool none = (begins & ((2ull << i) - 1)) != 0;
+                o *= fade;
+                if (begins) {
+                    const bool none = (begins & ((2ull << i) - 1)) != 0;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) o[r] = none ? 0.0f : o[r] * fade;
+                    for (int r = 0; r < 4; ++r) o[r] = none ? 0.0f : o[r];
+                }
 #pragma unroll
                 for (int b = 0; b <= I / 2; ++b) {
                     bf16x8 x[MID];
@@ -401,9 +429,8 @@ struct Attention {
                     for (int m = 0; m < MID; ++m) x[m] = *(const bf16x8 *)&within[m][i * kWithin + 32 * b + 8 * quad];
                     o = multiply(values[b], x, o);
                 }
-                const int d = 16 * wave + 4 * quad;
                 if (a.out && i < n && d < a.values) {
-                    typename Element<TYPE>::one *const to = (typename Element<TYPE>::one *)a.out + out_at + c.tick(i) * a.os.tick + d;
+                    typename Element<TYPE>::one *const to = out + 16 * I * step;
                     if (d + 4 <= a.values) {
                         store_four<TYPE>(to, o);
                     } else {
@@ -414,6 +441,7 @@ struct Attention {
                 }
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
         // the values faded by the ticks behind theirs; those of episodes that have ended count no more
         const int newest = begins ? 63 - __builtin_clzll(begins) : 0;
         const float left = __builtin_amdgcn_exp2f(l2 * (float)n);
@@ -430,10 +458,19 @@ struct Attention {
                                           : __builtin_shufflevector(values[b][p], values[b][p], 0, 1, 2, 3);
                     x += __builtin_convertvector(y, f32x4);
                 }
+                const int first = 32 * b + 16 * half + 4 * quad;
+                if (n == C) {
+                    const float fade = __builtin_amdgcn_exp2f(l2 * (float)(C - 4 - first + a.backward)) * a.scale_added;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int j = 32 * b + 16 * half + 4 * quad + r;
-                    x[r] = j >= newest && j < n ? x[r] * (__builtin_amdgcn_exp2f(l2 * (float)(n - 1 - j + a.backward)) * a.scale_added) : 0.0f;
+                    for (int r = 0; r < 4; ++r) x[r] *= fade * power[3 - r];
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        x[r] = first + r < n ? x[r] * (__builtin_amdgcn_exp2f(l2 * (float)(n - 1 - first - r + a.backward)) * a.scale_added) : 0.0f;
+                }
+                if (begins) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[r] = first + r >= newest ? x[r] : 0.0f;
                 }
                 split(part[half], x);
             }
@@ -442,9 +479,8 @@ struct Attention {
         }
 #pragma unroll
         for (int s = 0; s < TILES; ++s) {
-            f32x4 x;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] = begins ? 0.0f : state[s][r] * left;
+            f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (!begins) x = state[s] * left;
 #pragma unroll
             for (int b = 0; b < C / 32; ++b) {
                 if (32 * b >= n) break;
@@ -471,10 +507,11 @@ struct Attention {
             float sum = 0.0f;
 #pragma unroll
             for (int s = 0; s < TILES; ++s) {
-                asm volatile("" ::: "memory");     // a few loads at a time: this path is to cost no registers
+                int first = 4 * quad;              // a few loads at a time, their places not worked out beforehand: this
+                asm volatile("" : "+v"(first) : : "memory");       // path is to cost no registers
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int key = 16 * s + 4 * quad + r;
+                    const int key = 16 * s + first + r;
                     float x = begun ? 0.0f : a.backward ? state[s][r] : state[s][r] * e;
                     if (key < a.keys) {
                         x = fmaf(element<TYPE>(a.k, k_at + t * a.ks.tick + key), value, x);
@@ -493,6 +530,11 @@ struct Attention {
     }
 };
 
+__device__ __forceinline__ int64_t uniform(int64_t v)
+{
+    return (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)v) | (int64_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32;
+}
+
 // Workgroups are dealt to the eight XCDs in turn: each takes a run of neighbours, which share lines.
 __device__ __forceinline__ int64_t neighbour(int64_t id, int64_t all)
 {
@@ -503,7 +545,7 @@ __device__ __forceinline__ int64_t neighbour(int64_t id, int64_t all)
 // A workgroup has a row's head, or a segment of its ticks, and goes through the chunks with the state in registers; the
 // next chunk's rows are under way while it works on the present one.  CARRY: nothing is read, the states that the segments
 // would leave of nothing are.
-constexpr int attention_wavefronts(int d) { return 2; }   // of a SIMD
+constexpr int attention_wavefronts(int d) { return d == 128 ? 2 : d == 64 ? 3 : 4; }   // of a SIMD
 
 template <int D, int TYPE, bool CARRY>
 __global__ __launch_bounds__(4 * D, attention_wavefronts(D)) void tabx_attention_kernel(const AttentionArgs a)
@@ -513,17 +555,20 @@ __global__ __launch_bounds__(4 * D, attention_wavefronts(D)) void tabx_attention
     __shared__ typename A::In q, k, v;
     __shared__ __bf16 within[A::MID][C * A::kWithin];
     __shared__ int wild[2];                                    // of this chunk and the one before: not all is finite
-    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     int turn = 0;
     for (int64_t id = blockIdx.x; id < a.works; id += gridDim.x) {
         const int64_t w = a.works <= gridDim.x ? neighbour(id, a.works) : id;
-        const int segment = (int)(w % a.segments);
-        const int64_t rh = w / a.segments, r = rh / a.heads;
-        const int h = (int)(rh % a.heads);
+        // (a division's result is the same for all, but not known to be)
+        const int64_t rh = a.segments == 1 ? w : uniform(w / a.segments);
+        const int segment = (int)(w - rh * a.segments);
+        const int64_t r = __builtin_amdgcn_readfirstlane((int)((uint32_t)rh / (uint32_t)a.heads));       // (rows x heads has 31 bits)
+        const int h = (int)(rh - r * a.heads);
         const int64_t first = segment * a.segment, last = min(first + a.segment, a.ticks);
-        const int64_t env = r / a.units;
+        const int64_t env = __builtin_amdgcn_readfirstlane((int)((uint32_t)r / (uint32_t)a.units));
         const int64_t q_at = r * a.qs.row + h * a.qs.head, k_at = r * a.ks.row + h * a.ks.head, v_at = r * a.vs.row + h * a.vs.head,
                       out_at = r * a.os.row + h * a.os.head;
+        if (CARRY && segment == a.segments - 1) continue;      // (nothing comes behind it)
         if (a.controlled && a.controlled[r] == 0) {
             if (CARRY || !a.zero_out) continue;
             for (int64_t t = first; a.out && t < last; ++t)
@@ -534,30 +579,39 @@ __global__ __launch_bounds__(4 * D, attention_wavefronts(D)) void tabx_attention
                     a.state_out[rh * a.keys * a.values + (j / a.values) * a.state_key + (j % a.values) * a.state_value] = 0.0f;
             continue;
         }
-        const float l2 = fmaxf(log2_decay(a.log_decay, h), -1e9f);     // (all at once, and none of no ticks)
-        // a lane's elements of a state, as offsets that are worked out where they are needed and not kept meanwhile
-        const auto each = [&](int64_t along_keys, int64_t along_values, auto visit) {
+        const float decay = fmaxf(log2_decay(a.log_decay, h), -1e9f);  // (all at once, and none of no ticks)
+        // a lane's elements of a state, as offsets from a place that is the same for all; worked out where they are needed
+        // and not kept meanwhile
+        const auto each = [&](int along_keys, int along_values, auto visit) {
             int here = 0;
             asm volatile("" : "+v"(here));
-            const int value = 16 * wave + col + here, first_key = 4 * quad + here;
+            const int value = 16 * wave + (lane & 15) + here, first_key = 4 * (lane >> 4) + here, at = first_key * along_keys + value * along_values;
+            if (a.keys == D && a.values == D) {
 #pragma unroll
-            for (int s = 0; s < A::TILES; ++s)
+                for (int s = 0; s < A::TILES; ++s)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int key = first_key + 16 * s + i;
-                    if (key < a.keys && value < a.values) visit(s, i, key * (int)along_keys + value * (int)along_values);
-                }
+                    for (int i = 0; i < 4; ++i) visit(s, i, (16 * s + i) * along_keys, at);
+            } else if (value < a.values) {
+#pragma unroll
+                for (int s = 0; s < A::TILES; ++s)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (first_key + 16 * s + i < a.keys) visit(s, i, (16 * s + i) * along_keys, at);
+            }
         };
         typename A::State state;
 #pragma unroll
         for (int s = 0; s < A::TILES; ++s) state[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         if (!CARRY && a.carried) {
             const float *const from = a.carried + w * a.keys * a.values;
-            each(a.values, 1, [&](int s, int i, int at) { state[s][i] = from[at]; });
+            each(a.values, 1, [&](int s, int i, int from_there, int at) { state[s][i] = (from + from_there)[at]; });
         } else if (!CARRY && a.state_in) {
             const float *const from = a.state_in + rh * a.keys * a.values;
-            each(a.state_key, a.state_value, [&](int s, int i, int at) { state[s][i] = from[at]; });
+            each((int)a.state_key, (int)a.state_value, [&](int s, int i, int from_there, int at) { state[s][i] = (from + from_there)[at]; });
         }
+        float power[4];                            // of the decay, for 0 to 3 ticks
+#pragma unroll
+        for (int i = 0; i < 4; ++i) power[i] = __builtin_amdgcn_exp2f(decay * (float)i);
         float kept = 1.0f;
         typename A::Rows qr, kr, vr;
         int flag = 0;
@@ -578,6 +632,10 @@ __global__ __launch_bounds__(4 * D, attention_wavefronts(D)) void tabx_attention
         for (int64_t begin = first; begin < last; begin += C) {
             const int n = (int)min((int64_t)C, last - begin);
             const Course here = next;
+            // powers and places are worked out for every chunk: kept, they would cost a wavefront
+            float l2 = decay;
+            int col = lane & 15, quad = lane >> 4;
+            asm volatile("" : "+v"(l2), "+v"(col), "+v"(quad));
             turn ^= 1;
             if (threadIdx.x == 0) wild[turn] = 0;
             __syncthreads();                                   // the chunk before has been worked on
@@ -589,11 +647,11 @@ __global__ __launch_bounds__(4 * D, attention_wavefronts(D)) void tabx_attention
             if (next.begin < last) fetch((int)min((int64_t)C, last - next.begin));
             __syncthreads();
             if constexpr (!CARRY) {
-                A::compare(within, q, k, begins, l2, a.scale_within, wave, col, quad);
+                A::compare(within, q, k, begins, l2, power, a.scale_within, wave, col, quad);
                 __syncthreads();
             }
             if (__builtin_expect(wild[turn], 0)) A::template advance_slowly<!CARRY>(state, begins, n, l2, a, here, q_at, k_at, v_at, out_at, wave, col, quad);
-            else A::template advance<!CARRY>(state, within, q, k, v, begins, n, l2, a, here, out_at, wave, col, quad);
+            else A::template advance<!CARRY>(state, within, q, k, v, begins, n, l2, power, a, here, out_at, wave, col, quad);
             kept = begins || kept < 0.0f ? -1.0f : kept * __builtin_amdgcn_exp2f(l2 * (float)n);
         }
         float *const to = CARRY ? a.carried + w * a.keys * a.values : segment == a.segments - 1 ? a.state_out : nullptr;
@@ -602,10 +660,10 @@ __global__ __launch_bounds__(4 * D, attention_wavefronts(D)) void tabx_attention
         // backwards, what is left for the state before the first tick, if that belongs to its episode
         const bool cut = !CARRY && a.backward && a.fresh && a.ticks > 0 && a.fresh[env] != 0;
         if (CARRY) {
-            each(a.values, 1, [&](int s, int i, int at) { to[at] = state[s][i]; });
+            each(a.values, 1, [&](int s, int i, int from_there, int at) { (to + from_there)[at] = state[s][i]; });
         } else {
             float *const of = to + rh * a.keys * a.values;
-            each(a.state_key, a.state_value, [&](int s, int i, int at) { of[at] = cut ? 0.0f : state[s][i]; });
+            each((int)a.state_key, (int)a.state_value, [&](int s, int i, int from_there, int at) { (of + from_there)[at] = cut ? 0.0f : state[s][i]; });
         }
     }
 }
@@ -613,16 +671,24 @@ __global__ __launch_bounds__(4 * D, attention_wavefronts(D)) void tabx_attention
 // The states that the segments leave become those before them, one behind the other: a thread per element.
 static __global__ __launch_bounds__(256) void tabx_attention_join_kernel(const AttentionArgs a)
 {
+    constexpr int AHEAD = 16;
     const int64_t size = (int64_t)a.keys * a.values, all = a.rows * a.heads * size;
     for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < all; at += (int64_t)gridDim.x * 256) {
         const int64_t rh = at / size, d = at % size;
         if (a.controlled && a.controlled[rh / a.heads] == 0) continue;
         float s = a.state_in ? a.state_in[rh * size + d / a.values * a.state_key + d % a.values * a.state_value] : 0.0f;
-        for (int n = 0; n < a.segments; ++n) {
-            float *const here = a.carried + (rh * a.segments + n) * size + d;
-            const float left = *here, kept = a.kept[rh * a.segments + n];
-            *here = s;
-            s = kept < 0.0f ? left : fmaf(kept, s, left);
+        float *const of = a.carried + rh * a.segments * size + d;
+        const float *const kept = a.kept + rh * a.segments;
+        for (int n = 0; n < a.segments; n += AHEAD) {          // (what the last one leaves is the attention's to work out)
+            float left[AHEAD];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) left[i] = n + i < a.segments - 1 ? of[(n + i) * size] : 0.0f;
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                if (n + i >= a.segments) break;
+                of[(n + i) * size] = s;
+                if (n + i < a.segments - 1) s = kept[n + i] < 0.0f ? left[i] : fmaf(kept[n + i], s, left[i]);
+            }
         }
     }
 }

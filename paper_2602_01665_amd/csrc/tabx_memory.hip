@@ -158,21 +158,40 @@ static Strides strides_of(const TabxHeads &m) { return Strides{m.tick_stride, m.
 
 // --- rotation -----------------------------------------------------------------------------------
 
-template <int TYPE, bool INTERLEAVED, int LANES>
-static int launch_rotary(const RotaryArgs &a, void *stream)
+// at / divisor as the upper half of at x magic, for both below 2^16.
+static uint32_t magic_of(int64_t divisor, int64_t most) { return divisor >= 2 && divisor < 65536 && most < 65536 ? (uint32_t)(((int64_t)1 << 32) / divisor + 1) : 0; }
+
+template <int TYPE, int PAIRS, bool FAR>
+static int launch_rotary(const RotaryArgs &a, bool interleaved, void *stream)
 {
-    return launch(tabx_rotary_kernel<LANES, TYPE, INTERLEAVED>, least(quotient_up(a.rows, 256 / LANES), kMostGroups), 256, a, stream);
+    const int64_t groups = least(quotient_up(a.rows, a.group_rows), kMostGroups);
+    return launch(interleaved ? tabx_rotary_kernel<TYPE, PAIRS, true, FAR> : tabx_rotary_kernel<TYPE, PAIRS, false, FAR>, groups, 256, a, stream);
 }
 
-template <int TYPE, bool INTERLEAVED>
-static int rotary(const RotaryArgs &a, void *stream)
+template <int TYPE, int PAIRS>
+static int rotary_in_runs(RotaryArgs a, bool interleaved, bool copies, void *stream)
 {
-    const int lanes = (a.pairs + 3) / 4;
-    if (lanes <= 4) return launch_rotary<TYPE, INTERLEAVED, 4>(a, stream);
-    if (lanes <= 8) return launch_rotary<TYPE, INTERLEAVED, 8>(a, stream);
-    if (lanes <= 16) return launch_rotary<TYPE, INTERLEAVED, 16>(a, stream);
-    if (lanes <= 32) return launch_rotary<TYPE, INTERLEAVED, 32>(a, stream);
-    return launch_rotary<TYPE, INTERLEAVED, 64>(a, stream);
+    const int64_t runs = quotient_up(a.pairs, PAIRS), slots = runs + (copies ? quotient_up(a.width - 2 * a.pairs, PAIRS) : 0);
+    if (a.heads > INT32_MAX / (2 * slots)) return TABX_ERR_SHAPE;
+    a.row_angles = (int32_t)(runs * PAIRS);
+    a.head_slots = (int32_t)slots, a.row_slots = (int32_t)(slots * a.heads);
+    int64_t rows = 1024 / a.row_slots;             // four runs to a lane
+    rows = least(rows < 1 ? 1 : rows, kRotaryAngles / a.row_angles);
+    a.group_rows = (int32_t)rows;
+    a.row_magic = magic_of(a.row_slots, rows * a.row_slots);
+    a.head_magic = magic_of(a.head_slots, a.row_slots);
+    a.angle_magic = magic_of(a.row_angles, rows * a.row_angles);
+    const int64_t near = ((int64_t)1 << 30) - a.width;
+    const bool far = a.x_row > near / rows || a.y_row > near / rows || a.x_head > near / a.heads || a.y_head > near / a.heads;
+    return far ? launch_rotary<TYPE, PAIRS, true>(a, interleaved, stream) : launch_rotary<TYPE, PAIRS, false>(a, interleaved, stream);
+}
+
+static int rotary(const RotaryArgs &a, int type, bool interleaved, bool copies, void *stream)
+{
+    const bool eight = a.pairs % 8 == 0 && a.width % 8 == 0;       // 16 bytes of 16-bit elements
+    if (type == TABX_F32) return rotary_in_runs<TABX_F32, 4>(a, interleaved, copies, stream);
+    if (type == TABX_BF16) return eight ? rotary_in_runs<TABX_BF16, 8>(a, interleaved, copies, stream) : rotary_in_runs<TABX_BF16, 4>(a, interleaved, copies, stream);
+    return eight ? rotary_in_runs<TABX_F16, 8>(a, interleaved, copies, stream) : rotary_in_runs<TABX_F16, 4>(a, interleaved, copies, stream);
 }
 
 // --- linear attention ---------------------------------------------------------------------------
@@ -380,11 +399,8 @@ int tabx_rotary(int64_t rows, int32_t heads, int32_t width, const TabxHeads *x, 
     a.row_mask = row_mask;
     a.frequency = frequency;
     a.rows = rows, a.heads = heads, a.width = width;
-    a.num_axes = num_axes, a.sign = inverse ? -1.0 : 1.0;
-    a.copies = x->data != y->data;
-    if (x->type == TABX_F32) return interleaved ? rotary<TABX_F32, true>(a, stream) : rotary<TABX_F32, false>(a, stream);
-    if (x->type == TABX_BF16) return interleaved ? rotary<TABX_BF16, true>(a, stream) : rotary<TABX_BF16, false>(a, stream);
-    return interleaved ? rotary<TABX_F16, true>(a, stream) : rotary<TABX_F16, false>(a, stream);
+    a.num_axes = num_axes, a.sign = (inverse ? -1.0 : 1.0) * 0.63661977236758134;
+    return rotary(a, x->type, interleaved != 0, x->data != y->data, stream);
 }
 
 int tabx_linear_attention_step(int64_t rows, int32_t heads, int32_t key_width, int32_t value_width, const TabxHeads *q,

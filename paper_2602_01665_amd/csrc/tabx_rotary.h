@@ -1,5 +1,7 @@
 // Rotation of pairs of a head's elements by angles that grow along several axes.
 #pragma once
+#include <type_traits>
+
 #include "tabx_rows.h"
 
 #pragma clang fp contract(off)
@@ -15,8 +17,10 @@ struct RotaryArgs {
     int64_t     rows, x_row, x_head, y_row, y_head;   // strides in elements
     int32_t     axis_type[TABX_ROTARY_MAX_AXES], units[TABX_ROTARY_MAX_AXES], end[TABX_ROTARY_MAX_AXES];   // end: of its pairs
     int32_t     num_axes, heads, width, pairs;
-    int32_t     copies;            // the elements behind the pairs are copied (y is not x itself)
-    double      sign;              // of the angles
+    int32_t     group_rows, row_angles;               // rows of a workgroup; angles of a row in LDS, whole runs
+    int32_t     row_slots, head_slots;                // runs of pairs or copied elements of a row, of a head
+    uint32_t    row_magic, head_magic, angle_magic;   // 2^32 / row_slots, head_slots, angles of a row, rounded up; 0: divide
+    double      sign;              // of the angles, times the quarter turns of a radian
 };
 
 // Cosine and sine of an angle given in quarter turns: the nearest whole number of them is taken off in 64 bits, what is
@@ -37,123 +41,150 @@ __device__ __forceinline__ void quarter_turns(double quarters, float &cosine, fl
     sine = turn & 2 ? -d : d;
 }
 
-// Four elements (or fewer) of one kind of a pair, `step` apart.
-template <int TYPE, int STEP>
-__device__ __forceinline__ void load_some(f32x4 &v, const typename Element<TYPE>::one *at, int count)
-{
-    if (STEP == 1 && count == 4) {
-        v = load_four<TYPE>(at);
-    } else {
+// N elements as they lie in memory, from `at` on, wherever that lies, and in 32 bits.
+template <int TYPE, int N>
+struct Run {
+    typedef typename Element<TYPE>::one T;
+    typedef T Raw __attribute__((ext_vector_type(N)));
+    typedef Raw Anywhere __attribute__((aligned(sizeof(T))));
+    typedef float Floats __attribute__((ext_vector_type(N)));
+    Raw v;
+    __device__ __forceinline__ void load(const T *at) { v = *(const Anywhere *)at; }
+    __device__ __forceinline__ void load_some(const T *at, int step, int count)
+    {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = i < count ? (float)at[i * STEP] : 0.0f;
+        for (int i = 0; i < N; ++i) v[i] = i < count ? at[i * step] : (T)0.0f;
     }
-}
-
-template <int TYPE, int STEP>
-__device__ __forceinline__ void store_some(typename Element<TYPE>::one *at, f32x4 v, int count)
-{
-    if (STEP == 1 && count == 4) {
-        store_four<TYPE>(at, v);
-    } else {
+    __device__ __forceinline__ void store(T *at) const { *(Anywhere *)at = v; }
+    __device__ __forceinline__ void store_some(T *at, int step, int count) const
+    {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < count) at[i * STEP] = (typename Element<TYPE>::one)v[i];
+        for (int i = 0; i < N; ++i)
+            if (i < count) at[i * step] = v[i];
     }
-}
+};
 
-// Four pairs (or fewer): the first elements in u, the second ones in v.
-template <int TYPE, bool INTERLEAVED>
-__device__ __forceinline__ void load_pairs(f32x4 &u, f32x4 &v, const typename Element<TYPE>::one *x, int first, int pairs, int count)
-{
-    if constexpr (!INTERLEAVED) {
-        load_some<TYPE, 1>(u, x + first, count);
-        load_some<TYPE, 1>(v, x + pairs + first, count);
-    } else if (count == 4) {
-        const f32x4 a = load_four<TYPE>(x + 2 * first), b = load_four<TYPE>(x + 2 * first + 4);
-        u = __builtin_shufflevector(a, b, 0, 2, 4, 6), v = __builtin_shufflevector(a, b, 1, 3, 5, 7);
-    } else {
-        load_some<TYPE, 2>(u, x + 2 * first, count);
-        load_some<TYPE, 2>(v, x + 2 * first + 1, count);
-    }
-}
+// A workgroup takes some rows: it works out their angles, once for all heads, and then goes through their heads in the order
+// of memory, PAIRS pairs (or as many of the elements that are copied) to a lane, with the loads of the first of them under
+// way meanwhile.  FAR: a workgroup's rows span more than 2^31 elements.
+constexpr int kRotaryAngles = 2048;                // of a workgroup: 16 KB of LDS
 
-template <int TYPE, bool INTERLEAVED>
-__device__ __forceinline__ void store_pairs(f32x4 u, f32x4 v, typename Element<TYPE>::one *y, int first, int pairs, int count)
-{
-    if constexpr (!INTERLEAVED) {
-        store_some<TYPE, 1>(y + first, u, count);
-        store_some<TYPE, 1>(y + pairs + first, v, count);
-    } else if (count == 4) {
-        store_four<TYPE>(y + 2 * first, __builtin_shufflevector(u, v, 0, 4, 1, 5));
-        store_four<TYPE>(y + 2 * first + 4, __builtin_shufflevector(u, v, 2, 6, 3, 7));
-    } else {
-        store_some<TYPE, 2>(y + 2 * first, u, count);
-        store_some<TYPE, 2>(y + 2 * first + 1, v, count);
-    }
-}
-
-// LANES of a wavefront share a row, each with four of its pairs, whose angles serve all of the row's heads; HEADS of them are
-// on their way at a time.
-template <int LANES, int TYPE, bool INTERLEAVED>
+template <int TYPE, int PAIRS, bool INTERLEAVED, bool FAR>
 __global__ __launch_bounds__(256) void tabx_rotary_kernel(const RotaryArgs a)
 {
     typedef typename Element<TYPE>::one T;
-    constexpr int ROWS = 256 / LANES;              // of a workgroup at a time
-    constexpr int HEADS = 4;
-    const int lane = (int)threadIdx.x % LANES, first = 4 * lane;
-    const int count = max(0, min(4, a.pairs - first));
-    double frequency[4];
-    int axis[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int p = min(first + i, a.pairs - 1);
-        frequency[i] = a.frequency[p] * (a.sign * 0.63661977236758134);       // quarter turns
-        axis[i] = 0;
-#pragma unroll
-        for (int n = 1; n < TABX_ROTARY_MAX_AXES; ++n) axis[i] += n < a.num_axes && p >= a.end[n - 1];
-    }
-    const int behind = a.width - 2 * a.pairs;
-    for (int64_t r = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES; r < a.rows; r += (int64_t)gridDim.x * ROWS) {
-        if (a.row_mask && a.row_mask[r] == 0) continue;
-        const T *x = (const T *)a.x + r * a.x_row;
-        T *y = (T *)a.y + r * a.y_row;
-        f32x4 u[HEADS], v[HEADS];
-        const auto fetch = [&](int h) {
-#pragma unroll
-            for (int n = 0; n < HEADS; ++n) load_pairs<TYPE, INTERLEAVED>(u[n], v[n], x + min(h + n, a.heads - 1) * a.x_head, first, a.pairs, count);
-        };
-        fetch(0);
-        double where[TABX_ROTARY_MAX_AXES];
-#pragma unroll
-        for (int n = 0; n < TABX_ROTARY_MAX_AXES; ++n) {
-            where[n] = 0.0;
-            if (n >= a.num_axes) continue;
-            const int64_t at = a.units[n] == 1 ? r : r >> 32 ? r / a.units[n] : (int64_t)((uint32_t)r / (uint32_t)a.units[n]);
-            where[n] = a.axis_type[n] == TABX_I32 ? (double)((const int32_t *)a.position[n])[at] : (double)((const float *)a.position[n])[at];
-        }
-        float cosine[4], sine[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const double p = axis[i] == 0 ? where[0] : axis[i] == 1 ? where[1] : axis[i] == 2 ? where[2] : where[3];
-            quarter_turns(p * frequency[i], cosine[i], sine[i]);
-        }
-        for (int h = 0; h < a.heads; h += HEADS) {
-            if (h > 0) fetch(h);
-#pragma unroll
-            for (int n = 0; n < HEADS; ++n) {
-                if (h + n >= a.heads) break;
-                f32x4 s, t;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    s[i] = fmaf(u[n][i], cosine[i], -(v[n][i] * sine[i]));
-                    t[i] = fmaf(u[n][i], sine[i], v[n][i] * cosine[i]);
+    typedef Run<TYPE, PAIRS> R;
+    typedef typename R::Floats F;
+    typedef std::conditional_t<FAR, int64_t, int32_t> Offset;
+    constexpr int AHEAD = 4;
+    __shared__ float cosines[kRotaryAngles], sines[kRotaryAngles];
+    const int turned = a.row_angles / PAIRS, behind = a.width - 2 * a.pairs;
+    for (int64_t base = (int64_t)blockIdx.x * a.group_rows; base < a.rows; base += (int64_t)gridDim.x * a.group_rows) {
+        const int rows = (int)min((int64_t)a.group_rows, a.rows - base);
+        const int units = rows * a.row_slots;
+        const T *const x = (const T *)a.x + base * a.x_row;
+        T *const y = (T *)a.y + base * a.y_row;
+        struct Unit {
+            R u, v;
+            Offset to;             // of its first element in y
+            int angle, count;      // count: of its pairs, or less than 0: of its copied elements; 0: none
+        } unit[AHEAD];
+        const auto fetch = [&](Unit &n, int at) {
+            n.count = 0;
+            if (at >= units) return;
+            const int row = a.row_magic ? (int)__umulhi((uint32_t)at, a.row_magic) : at / a.row_slots;
+            const int rest = at - row * a.row_slots;
+            const int head = a.head_magic ? (int)__umulhi((uint32_t)rest, a.head_magic) : rest / a.head_slots;
+            const int slot = rest - head * a.head_slots;
+            if (a.row_mask && a.row_mask[base + row] == 0) return;
+            const bool turns = slot < turned;
+            const int first = turns ? (INTERLEAVED ? 2 : 1) * PAIRS * slot : 2 * a.pairs + PAIRS * (slot - turned);
+            const T *const from = x + ((Offset)row * (Offset)a.x_row + (Offset)head * (Offset)a.x_head + first);
+            n.to = (Offset)row * (Offset)a.y_row + (Offset)head * (Offset)a.y_head + first;
+            n.angle = row * a.row_angles + PAIRS * slot;
+            if (turns) {
+                n.count = min(PAIRS, a.pairs - PAIRS * slot);
+                if (n.count == PAIRS) {            // (interleaved: the pairs' first half and second half)
+                    n.u.load(from);
+                    n.v.load(from + (INTERLEAVED ? PAIRS : a.pairs));
+                } else {
+                    n.u.load_some(from, INTERLEAVED ? 2 : 1, n.count);
+                    n.v.load_some(from + (INTERLEAVED ? 1 : a.pairs), INTERLEAVED ? 2 : 1, n.count);
                 }
-                store_pairs<TYPE, INTERLEAVED>(s, t, y + (h + n) * a.y_head, first, a.pairs, count);
+            } else {
+                const int some = min(PAIRS, behind - PAIRS * (slot - turned));
+                n.count = -some;
+                if (some == PAIRS) n.u.load(from);
+                else n.u.load_some(from, 1, some);
             }
+        };
+        const auto finish = [&](Unit &n) {
+            T *const to = y + n.to;
+            if (n.count > 0) {
+                F u = __builtin_convertvector(n.u.v, F), v = __builtin_convertvector(n.v.v, F);
+                if (INTERLEAVED && n.count == PAIRS) {
+                    const F s = u, t = v;
+#pragma unroll
+                    for (int i = 0; i < PAIRS; ++i) {
+                        u[i] = 2 * i < PAIRS ? s[2 * i % PAIRS] : t[2 * i % PAIRS];
+                        v[i] = 2 * i < PAIRS ? s[(2 * i + 1) % PAIRS] : t[(2 * i + 1) % PAIRS];
+                    }
+                }
+                F first, second;
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) {
+                    const float c = cosines[n.angle + i], s = sines[n.angle + i];
+                    first[i] = fmaf(u[i], c, -(v[i] * s));
+                    second[i] = fmaf(u[i], s, v[i] * c);
+                }
+                if (n.count == PAIRS) {
+                    if (INTERLEAVED) {
+                        const F s = first, t = second;
+#pragma unroll
+                        for (int i = 0; i < PAIRS; ++i) {
+                            first[i] = i % 2 ? t[i / 2] : s[i / 2];
+                            second[i] = i % 2 ? t[(PAIRS + i) / 2] : s[(PAIRS + i) / 2];
+                        }
+                    }
+                    n.u.v = __builtin_convertvector(first, typename R::Raw), n.v.v = __builtin_convertvector(second, typename R::Raw);
+                    n.u.store(to);
+                    n.v.store(to + (INTERLEAVED ? PAIRS : a.pairs));
+                } else {
+                    n.u.v = __builtin_convertvector(first, typename R::Raw), n.v.v = __builtin_convertvector(second, typename R::Raw);
+                    n.u.store_some(to, INTERLEAVED ? 2 : 1, n.count);
+                    n.v.store_some(to + (INTERLEAVED ? 1 : a.pairs), INTERLEAVED ? 2 : 1, n.count);
+                }
+            } else if (n.count == -PAIRS) {
+                n.u.store(to);
+            } else if (n.count < 0) {
+                n.u.store_some(to, 1, -n.count);
+            }
+        };
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n) fetch(unit[n], (int)threadIdx.x + 256 * n);
+        for (int at = threadIdx.x; at < rows * a.row_angles; at += 256) {
+            const int row = a.angle_magic ? (int)__umulhi((uint32_t)at, a.angle_magic) : at / a.row_angles;
+            const int pair = min(at - row * a.row_angles, a.pairs - 1);
+            int axis = 0;
+#pragma unroll
+            for (int n = 1; n < TABX_ROTARY_MAX_AXES; ++n) axis += n < a.num_axes && pair >= a.end[n - 1];
+            const void *const position = axis == 0 ? a.position[0] : axis == 1 ? a.position[1] : axis == 2 ? a.position[2] : a.position[3];
+            const int units_of = axis == 0 ? a.units[0] : axis == 1 ? a.units[1] : axis == 2 ? a.units[2] : a.units[3];
+            const int type = axis == 0 ? a.axis_type[0] : axis == 1 ? a.axis_type[1] : axis == 2 ? a.axis_type[2] : a.axis_type[3];
+            const int64_t r = base + row;
+            const int64_t where = units_of == 1 ? r : r >> 32 ? r / units_of : (int64_t)((uint32_t)r / (uint32_t)units_of);
+            const uint32_t raw = ((const uint32_t *)position)[where];
+            const double p = type == TABX_I32 ? (double)(int32_t)raw : (double)__uint_as_float(raw);
+            quarter_turns(p * (a.frequency[pair] * a.sign), cosines[at], sines[at]);
         }
-        if (a.copies)
-            for (int h = 0; h < a.heads; ++h)
-                for (int j = lane; j < behind; j += LANES) y[h * a.y_head + 2 * a.pairs + j] = x[h * a.x_head + 2 * a.pairs + j];
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n) finish(unit[n]);
+        for (int at = (int)threadIdx.x + 256 * AHEAD; at < units; at += 256) {
+            fetch(unit[0], at);
+            finish(unit[0]);
+        }
+        __syncthreads();                           // the angles have been read
     }
 }
 
