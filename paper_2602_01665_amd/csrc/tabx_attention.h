@@ -11,6 +11,8 @@
 // grad_out.  Backwards, e has been applied to D before a chunk's last tick reads it, so the powers are e^i there and
 // e^(C-j) in D'; and an episode begins behind the tick where, forwards, the next one does.
 #pragma once
+#include <type_traits>
+
 #include "tabx_rows.h"
 
 #pragma clang fp contract(off)
@@ -25,7 +27,7 @@ struct Strides {
 
 struct AttentionArgs {
     const void *q, *k, *v;
-    void       *out;               // or nullptr
+    void       *out;
     Strides     qs, ks, vs, os;
     const float *log_decay;
     const uint8_t *fresh;          // [ticks][rows / units], or nullptr
@@ -34,12 +36,26 @@ struct AttentionArgs {
     float      *state_out;         // or nullptr
     float      *carried;           // [row and head][segment][keys][values]: states before each segment, or nullptr
     float      *kept;              // [row and head][segment]: what a segment leaves of the state before it; -1: an episode begins in it
-    int64_t     ticks, rows, envs, works, state_key, state_value;   // works: rows x heads x segments; strides of a state's elements
+    int64_t     ticks, rows, envs, works;   // works: rows x heads x segments
     int64_t     segment;           // ticks of a segment, a multiple of the chunk
-    int32_t     segments, heads, units, keys, values, type;
+    int32_t     segments, heads, units, keys, values;
     int32_t     backward;          // in time
-    int32_t     zero_out;          // rows that are not controlled get zeros (gradients)
-    float       scale_within, scale_state, scale_added;
+    float       scale_read, scale_added;   // of what is read, of what is taken in
+};
+
+// The way back: all that the three attentions of the gradients need.
+struct AttentionGradArgs {
+    const void *q, *k, *v, *grad_out;
+    void       *grad_q, *grad_k, *grad_v;  // each may be nullptr
+    Strides     qs, ks, vs, os, gqs, gks, gvs;
+    const float *log_decay;
+    const uint8_t *fresh, *controlled;
+    const float *state_in, *grad_state_out;
+    float      *grad_state_in;     // or nullptr
+    const float *states, *grad_states;     // before each segment, forwards and backwards in time, or nullptr
+    int64_t     ticks, rows, envs, works, segment;
+    int32_t     segments, heads, units, keys, values;
+    float       scale;
 };
 
 // exp(log_decay) and its powers as powers of two.
@@ -289,19 +305,46 @@ struct Tile {
     }
 };
 
-// One row's head (or a segment of its ticks) as an attention goes through it, and which way.
+// One row's head of an attention: its arrays from there on, strides of ticks, widths.
+struct Part {
+    const void *q, *k, *v;
+    void       *out;               // or nullptr
+    int64_t     q_tick, k_tick, v_tick, out_tick;
+    int         keys, values, backward;
+    float       scale_read, scale_added;
+};
+
+// The ticks that an attention goes through, in the direction of time taken, and where episodes begin in it.
 struct Course {
-    int64_t ticks, begin;          // of all; where the chunk at hand begins, counted in the direction of time taken
+    const uint8_t *fresh;          // of the row's env, or nullptr
+    int64_t envs, ticks, begin;    // begin: of the chunk at hand
     int     backward;
     __device__ __forceinline__ int64_t tick(int i) const { return backward ? ticks - 1 - (begin + i) : begin + i; }
+    // Backwards, an episode begins behind the tick where, forwards, the next one does.
+    __device__ __forceinline__ int begins(int i, int n) const
+    {
+        if (!fresh || i >= n) return 0;
+        const int64_t t = begin + i;
+        if (!backward) return fresh[t * envs];
+        return t > 0 ? fresh[(ticks - t) * envs] : 0;
+    }
 };
+
+template <typename T>
+__device__ __forceinline__ T *moved_on(T *data, int64_t elements, int bytes)
+{
+    typedef std::conditional_t<std::is_const_v<T>, const char, char> Byte;
+    return (T *)((Byte *)data + elements * bytes);
+}
 
 template <int D, int TYPE>
 struct Attention {
     static constexpr int C = chunk_of(D, TYPE), IN = Parts<TYPE>::in, MID = Parts<TYPE>::mid;
     static constexpr int WAVES = D / 16, THREADS = 64 * WAVES, PASSES = C * D / 8 / THREADS, TILES = D / 16;
+    typedef typename Element<TYPE>::one T;
     typedef Tile<D, C, IN> In;
     static constexpr int kWithin = C + 8;          // distance of rows of the products of queries and keys
+    typedef __bf16 Within[MID][C * kWithin];
 
     // A wavefront has 16 of the values and all of the state's lines of them, in the layout in which a product leaves its
     // result (a lane has four lines of one column), which is that of an operand of the next one (`along_results`).
@@ -309,12 +352,12 @@ struct Attention {
 
     struct Rows { Eight<TYPE> e[PASSES]; };
 
-    static __device__ __forceinline__ void load(Rows &rows, const void *data, int64_t at, int64_t tick, const Course &c, int n, int width)
+    static __device__ __forceinline__ void load(Rows &rows, const void *data, int64_t tick, const Course &c, int n, int width)
     {
         constexpr int across = D / 8;
         const int d = 8 * ((int)threadIdx.x % across), row = (int)threadIdx.x / across;
         const int64_t step = c.backward ? -tick : tick;
-        const typename Element<TYPE>::one *const from = (const typename Element<TYPE>::one *)data + at + c.tick(0) * tick + row * step + d;
+        const T *const from = (const T *)data + c.tick(0) * tick + row * step + d;
         if (n == C && width == D) {                // (the same for all: no lane has to be asked)
 #pragma unroll
             for (int p = 0; p < PASSES; ++p) rows.e[p].load(from + p * (THREADS / across) * step);
@@ -341,8 +384,8 @@ struct Attention {
     // Products of queries and keys, faded by the ticks between them, 0 where they do not belong together, in parts:
     // tiles of 16 x 16 on and below the diagonal, dealt to the wavefronts.  Rows are queries; along them the keys lie in the
     // order of `along_results`, so that a lane's eight are next to each other.
-    static __device__ __forceinline__ void compare(__bf16 (&within)[MID][C * kWithin], const In &q, const In &k, uint64_t begins, float l2,
-                                                   const float (&power)[4], float scale, int wave, int col, int quad)
+    static __device__ __forceinline__ void compare(Within &within, const In &q, const In &k, uint64_t begins, float l2, const float (&power)[4],
+                                                   float scale, int wave, int col, int quad)
     {
         constexpr int tiles = C / 16 * (C / 16 + 1) / 2;
         for (int tile = wave; tile < tiles; tile += WAVES) {
@@ -383,9 +426,9 @@ struct Attention {
 
     // What a chunk's queries read, and the state behind the chunk.
     template <bool READS>
-    static __device__ __forceinline__ void advance(State &state, const __bf16 (&within)[MID][C * kWithin], const In &q, const In &k, const In &v,
-                                                   uint64_t begins, int n, float l2, const float (&power)[4], const AttentionArgs &a,
-                                                   const Course &c, int64_t out_at, int wave, int col, int quad)
+    static __device__ __forceinline__ void advance(State &state, const Within &within, const In &q, const In &k, const In &v,
+                                                   uint64_t begins, int n, float l2, const float (&power)[4], const Part &a, const Course &c,
+                                                   int wave, int col, int quad)
     {
         bf16x8 values[C / 32][IN];                 // this lane's: 8 ticks of its column, of every 32
 #pragma unroll
@@ -401,11 +444,11 @@ struct Attention {
                 for (int m = 0; m < MID; ++m) held[s][m] = join(x[m], y[m]);
             }
             const int d = 16 * wave + 4 * quad;
-            const int64_t step = c.backward ? -a.os.tick : a.os.tick;
-            typename Element<TYPE>::one *const out = (typename Element<TYPE>::one *)a.out + out_at + c.tick(0) * a.os.tick + col * step + d;
+            const int64_t step = c.backward ? -a.out_tick : a.out_tick;
+            T *const out = (T *)a.out + c.tick(0) * a.out_tick + col * step + d;
 #pragma unroll
             for (int I = 0; I < C / 16; ++I) {
-                if (16 * I >= n) break;
+                if (16 * I >= n) continue;
                 __builtin_amdgcn_sched_barrier(0); // (operands of all of them at a time would not fit)
                 const int i = 16 * I + col;
                 f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -415,7 +458,7 @@ struct Attention {
                     q.along_results(x, 16 * I, 32 * s, col, quad);
                     o = multiply(held[s], x, o);
                 }
-                const float fade = __builtin_amdgcn_exp2f(l2 * (float)(i + 1 - a.backward)) * a.scale_state;
+                const float fade = __builtin_amdgcn_exp2f(l2 * (float)(i + 1 - a.backward)) * a.scale_read;
                 o *= fade;
                 if (begins) {
                     const bool none = (begins & ((2ull << i) - 1)) != 0;
@@ -430,13 +473,13 @@ struct Attention {
                     o = multiply(values[b], x, o);
                 }
                 if (a.out && i < n && d < a.values) {
-                    typename Element<TYPE>::one *const to = out + 16 * I * step;
+                    T *const to = out + 16 * I * step;
                     if (d + 4 <= a.values) {
                         store_four<TYPE>(to, o);
                     } else {
 #pragma unroll
                         for (int r = 0; r < 3; ++r)
-                            if (d + r < a.values) to[r] = (typename Element<TYPE>::one)o[r];
+                            if (d + r < a.values) to[r] = (T)o[r];
                     }
                 }
             }
@@ -483,7 +526,7 @@ struct Attention {
             if (!begins) x = state[s] * left;
 #pragma unroll
             for (int b = 0; b < C / 32; ++b) {
-                if (32 * b >= n) break;
+                if (32 * b >= n) continue;
                 bf16x8 y[IN];
                 k.across(y, 32 * b, 16 * s, col, quad);
                 x = multiply(y, faded[b], x);
@@ -495,15 +538,14 @@ struct Attention {
     // The same for a chunk with keys or values that are not finite, tick by tick: in a product of matrices they would reach
     // ticks that they do not belong to, as zero times them is not zero.
     template <bool READS>
-    static __device__ void advance_slowly(State &state, uint64_t begins, int n, float l2, const AttentionArgs &a, const Course &c,
-                                          int64_t q_at, int64_t k_at, int64_t v_at, int64_t out_at, int wave, int col, int quad)
+    static __device__ __forceinline__ void advance_slowly(State &state, uint64_t begins, int n, float l2, const Part &a, const Course &c, int wave, int col, int quad)
     {
         const float e = __builtin_amdgcn_exp2f(l2);
         const int d = 16 * wave + col;
         for (int i = 0; i < n; ++i) {
             const int64_t t = c.tick(i);
             const bool begun = begins >> i & 1;
-            const float value = d < a.values ? element<TYPE>(a.v, v_at + t * a.vs.tick + d) * a.scale_added : 0.0f;
+            const float value = d < a.values ? element<TYPE>(a.v, t * a.v_tick + d) * a.scale_added : 0.0f;
             float sum = 0.0f;
 #pragma unroll
             for (int s = 0; s < TILES; ++s) {
@@ -514,8 +556,8 @@ struct Attention {
                     const int key = 16 * s + first + r;
                     float x = begun ? 0.0f : a.backward ? state[s][r] : state[s][r] * e;
                     if (key < a.keys) {
-                        x = fmaf(element<TYPE>(a.k, k_at + t * a.ks.tick + key), value, x);
-                        if (READS) sum = fmaf(element<TYPE>(a.q, q_at + t * a.qs.tick + key), x, sum);
+                        x = fmaf(element<TYPE>(a.k, t * a.k_tick + key), value, x);
+                        if (READS) sum = fmaf(element<TYPE>(a.q, t * a.q_tick + key), x, sum);
                     }
                     state[s][r] = a.backward ? x * e : x;
                 }
@@ -524,8 +566,106 @@ struct Attention {
                 sum += __shfl_xor(sum, 16);
                 sum += __shfl_xor(sum, 32);
                 if (a.out && quad == 0 && d < a.values)
-                    ((typename Element<TYPE>::one *)a.out)[out_at + t * a.os.tick + d] = (typename Element<TYPE>::one)(sum * a.scale_state);
+                    ((T *)a.out)[t * a.out_tick + d] = (T)(sum * a.scale_read);
             }
+        }
+    }
+
+    // A lane's elements of a state in memory, elements along_keys and along_values apart.  Places are worked out from one
+    // that is the same for all, where they are needed.
+    static __device__ __forceinline__ void load_state(State &state, const float *from, int keys, int values, int along_keys, int along_values)
+    {
+        int lane = (int)threadIdx.x;
+        asm volatile("" : "+v"(lane));
+        const int value = 16 * (lane >> 6) + (lane & 15), first = 4 * (lane >> 4 & 3);
+        if (keys == D && values == D) {
+            const int at = first * along_keys + value * along_values;
+#pragma unroll
+            for (int s = 0; s < TILES; ++s)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) state[s][i] = (from + (16 * s + i) * along_keys)[at];
+        } else {
+            // beyond the widths, the last element: loads without a branch, which would be waited for one by one
+            const int column = min(value, values - 1) * along_values;
+#pragma unroll
+            for (int s = 0; s < TILES; ++s)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) state[s][i] = from[min(first + 16 * s + i, keys - 1) * along_keys + column];
+#pragma unroll
+            for (int s = 0; s < TILES; ++s)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) state[s][i] = first + 16 * s + i < keys && value < values ? state[s][i] : 0.0f;
+        }
+    }
+    static __device__ __forceinline__ void store_state(const State &state, float *to, int keys, int values, int along_keys, int along_values, bool zero)
+    {
+        int lane = (int)threadIdx.x;
+        asm volatile("" : "+v"(lane));
+        const int value = 16 * (lane >> 6) + (lane & 15), first = 4 * (lane >> 4 & 3), at = first * along_keys + value * along_values;
+        if (value >= values) return;
+#pragma unroll
+        for (int s = 0; s < TILES; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if ((keys == D) || first + 16 * s + i < keys) (to + (16 * s + i) * along_keys)[at] = zero ? 0.0f : state[s][i];
+    }
+    static __device__ __forceinline__ void clear(State &state)
+    {
+#pragma unroll
+        for (int s = 0; s < TILES; ++s) state[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+
+    struct Decay {
+        float l2, power[4];        // its logarithm, and what it leaves in 0 to 3 ticks
+        __device__ __forceinline__ Decay(const float *log_decay, int h)
+        {
+            l2 = fmaxf(log2_decay(log_decay, h), -1e9f);       // (all at once, and none of no ticks)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) power[i] = __builtin_amdgcn_exp2f(l2 * (float)i);
+        }
+    };
+
+    // One attention from tick `first` to `last`; the next chunk's rows are under way while it works on the present one.
+    // READS: queries are answered (else only the state goes on).  kept: what is left of the state before.  wild, turn: of the
+    // chunk at hand and the one before, whether not all of it is finite.
+    template <bool READS>
+    static __device__ __forceinline__ void go_through(State &state, float &kept, In &q, In &k, In &v, Within &within, int (&wild)[2], int &turn,
+                                                      const Part &a, Course next, int64_t last, const Decay &decay)
+    {
+        const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+        Rows qr, kr, vr;
+        int flag = 0;
+        const auto fetch = [&](int n) {
+            if constexpr (READS) load(qr, a.q, a.q_tick, next, n, a.keys);
+            load(kr, a.k, a.k_tick, next, n, a.keys);
+            load(vr, a.v, a.v_tick, next, n, a.values);
+            flag = next.begins(lane, n);
+        };
+        if (next.begin < last) fetch((int)min((int64_t)C, last - next.begin));
+        while (next.begin < last) {
+            const int n = (int)min((int64_t)C, last - next.begin);
+            const Course here = next;
+            // powers and places are worked out for every chunk: kept, they would cost a wavefront
+            float l2 = decay.l2;
+            int col = lane & 15, quad = lane >> 4;
+            asm volatile("" : "+v"(l2), "+v"(col), "+v"(quad));
+            turn ^= 1;
+            if (threadIdx.x == 0) wild[turn] = 0;
+            __syncthreads();                                   // the chunk before has been worked on
+            if constexpr (READS) store(q, qr);
+            const uint32_t odd = store(k, kr) | store(v, vr);
+            if (__ballot(odd != 0) && lane == 0) wild[turn] = 1;
+            const uint64_t begins = __ballot(flag != 0);       // bit i: an episode begins with the chunk's tick i
+            next.begin += C;
+            if (next.begin < last) fetch((int)min((int64_t)C, last - next.begin));
+            __syncthreads();
+            if constexpr (READS) {
+                compare(within, q, k, begins, l2, decay.power, a.scale_read * a.scale_added, wave, col, quad);
+                __syncthreads();
+            }
+            if (__builtin_expect(wild[turn], 0)) advance_slowly<READS>(state, begins, n, l2, a, here, wave, col, quad);
+            else advance<READS>(state, within, q, k, v, begins, n, l2, decay.power, a, here, wave, col, quad);
+            kept = begins || kept < 0.0f ? -1.0f : kept * __builtin_amdgcn_exp2f(l2 * (float)n);
         }
     }
 };
@@ -542,129 +682,166 @@ __device__ __forceinline__ int64_t neighbour(int64_t id, int64_t all)
     return x * run + (x < rest ? x : rest) + id / 8;
 }
 
-// A workgroup has a row's head, or a segment of its ticks, and goes through the chunks with the state in registers; the
-// next chunk's rows are under way while it works on the present one.  CARRY: nothing is read, the states that the segments
-// would leave of nothing are.
-constexpr int attention_wavefronts(int d) { return d == 128 ? 2 : d == 64 ? 3 : 4; }   // of a SIMD
+// What a workgroup works on: a row's head, or a segment of its ticks.
+struct Work {
+    int64_t at, rh, r, env;        // at: with its segment; rh: row and head
+    int     segment, h;
+    template <typename Args>
+    __device__ __forceinline__ Work(const Args &a, int64_t id)
+    {
+        at = a.works <= gridDim.x ? neighbour(id, a.works) : id;
+        // (a division's result is the same for all, but not known to be; rows x heads has 31 bits)
+        rh = a.segments == 1 ? at : uniform(at / a.segments);
+        segment = (int)(at - rh * a.segments);
+        r = __builtin_amdgcn_readfirstlane((int)((uint32_t)rh / (uint32_t)a.heads));
+        h = (int)(rh - r * a.heads);
+        env = __builtin_amdgcn_readfirstlane((int)((uint32_t)r / (uint32_t)a.units));
+    }
+    __device__ __forceinline__ int64_t of(const Strides &s) const { return r * s.row + h * s.head; }
+};
 
+// Wavefronts of a SIMD, as many as the LDS of a workgroup lets the machine hold.
+constexpr int attention_wavefronts(int d) { return d == 128 ? 2 : 3; }
+constexpr int attention_grad_wavefronts(int d) { return 2; }
+
+// A workgroup goes through its ticks with the state in registers.  CARRY: nothing is read, the states that the segments
+// would leave of nothing are.
 template <int D, int TYPE, bool CARRY>
 __global__ __launch_bounds__(4 * D, attention_wavefronts(D)) void tabx_attention_kernel(const AttentionArgs a)
 {
     typedef Attention<D, TYPE> A;
-    constexpr int C = A::C;
     __shared__ typename A::In q, k, v;
-    __shared__ __bf16 within[A::MID][C * A::kWithin];
-    __shared__ int wild[2];                                    // of this chunk and the one before: not all is finite
+    __shared__ typename A::Within within;
+    __shared__ int wild[2];
+    int turn = 0;
+    for (int64_t id = blockIdx.x; id < a.works; id += gridDim.x) {
+        const Work w(a, id);
+        if (CARRY && w.segment == a.segments - 1) continue;    // (nothing comes behind it)
+        if (a.controlled && a.controlled[w.r] == 0) continue;
+        constexpr int bytes = sizeof(typename A::T);
+        const Part part = {moved_on(a.q, w.of(a.qs), bytes), moved_on(a.k, w.of(a.ks), bytes), moved_on(a.v, w.of(a.vs), bytes),
+                           moved_on(a.out, w.of(a.os), bytes), a.qs.tick, a.ks.tick, a.vs.tick, a.os.tick, a.keys, a.values, a.backward,
+                           a.scale_read, a.scale_added};
+        const typename A::Decay decay(a.log_decay, w.h);
+        const int64_t size = a.keys * a.values;
+        typename A::State state;
+        if (!CARRY && a.carried) A::load_state(state, a.carried + w.at * size, a.keys, a.values, a.values, 1);
+        else if (!CARRY && a.state_in) A::load_state(state, a.state_in + w.rh * size, a.keys, a.values, a.values, 1);
+        else A::clear(state);
+        float kept = 1.0f;
+        const int64_t first = w.segment * a.segment;
+        A::template go_through<!CARRY>(state, kept, q, k, v, within, wild, turn, part,
+                                       Course{a.fresh ? a.fresh + w.env : nullptr, a.envs, a.ticks, first, a.backward}, min(first + a.segment, a.ticks), decay);
+        if (CARRY) {
+            A::store_state(state, a.carried + w.at * size, a.keys, a.values, a.values, 1, false);
+            if (threadIdx.x == 0) a.kept[w.at] = kept;
+        } else if (a.state_out && w.segment == a.segments - 1) {
+            A::store_state(state, a.state_out + w.rh * size, a.keys, a.values, a.values, 1, false);
+        }
+    }
+}
+
+// The gradients: forwards through the ticks for grad_q, then backwards for grad_k and grad_v, which read the same rows,
+// and the state's; the last chunk forwards is the first one backwards, and what was read is still in the caches.
+template <int D, int TYPE>
+__global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D)) void tabx_attention_grad_kernel(const AttentionGradArgs a)
+{
+    typedef Attention<D, TYPE> A;
+    typedef typename A::T T;
+    constexpr int C = A::C, bytes = sizeof(T);
+    __shared__ typename A::In q, k, v, g;
+    __shared__ typename A::Within within[2];
+    __shared__ int wild[2];
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     int turn = 0;
     for (int64_t id = blockIdx.x; id < a.works; id += gridDim.x) {
-        const int64_t w = a.works <= gridDim.x ? neighbour(id, a.works) : id;
-        // (a division's result is the same for all, but not known to be)
-        const int64_t rh = a.segments == 1 ? w : uniform(w / a.segments);
-        const int segment = (int)(w - rh * a.segments);
-        const int64_t r = __builtin_amdgcn_readfirstlane((int)((uint32_t)rh / (uint32_t)a.heads));       // (rows x heads has 31 bits)
-        const int h = (int)(rh - r * a.heads);
-        const int64_t first = segment * a.segment, last = min(first + a.segment, a.ticks);
-        const int64_t env = __builtin_amdgcn_readfirstlane((int)((uint32_t)r / (uint32_t)a.units));
-        const int64_t q_at = r * a.qs.row + h * a.qs.head, k_at = r * a.ks.row + h * a.ks.head, v_at = r * a.vs.row + h * a.vs.head,
-                      out_at = r * a.os.row + h * a.os.head;
-        if (CARRY && segment == a.segments - 1) continue;      // (nothing comes behind it)
-        if (a.controlled && a.controlled[r] == 0) {
-            if (CARRY || !a.zero_out) continue;
-            for (int64_t t = first; a.out && t < last; ++t)
-                for (int j = threadIdx.x; j < a.values; j += A::THREADS)
-                    ((typename Element<TYPE>::one *)a.out)[out_at + (a.backward ? a.ticks - 1 - t : t) * a.os.tick + j] = (typename Element<TYPE>::one)0.0f;
-            if (a.state_out && segment == a.segments - 1)
-                for (int j = threadIdx.x; j < a.keys * a.values; j += A::THREADS)
-                    a.state_out[rh * a.keys * a.values + (j / a.values) * a.state_key + (j % a.values) * a.state_value] = 0.0f;
+        const Work w(a, id);
+        const int64_t first = w.segment * a.segment, last = min(first + a.segment, a.ticks), size = a.keys * a.values;
+        T *const gq = (T *)a.grad_q + w.of(a.gqs), *const gk = (T *)a.grad_k + w.of(a.gks), *const gv = (T *)a.grad_v + w.of(a.gvs);
+        if (a.controlled && a.controlled[w.r] == 0) {
+            for (int64_t t = first; t < last; ++t)
+                for (int j = threadIdx.x; j < max(a.keys, a.values); j += A::THREADS) {
+                    if (a.grad_q && j < a.keys) gq[t * a.gqs.tick + j] = (T)0.0f;
+                    if (a.grad_k && j < a.keys) gk[t * a.gks.tick + j] = (T)0.0f;
+                    if (a.grad_v && j < a.values) gv[t * a.gvs.tick + j] = (T)0.0f;
+                }
+            if (a.grad_state_in && w.segment == 0)
+                for (int j = threadIdx.x; j < size; j += A::THREADS) a.grad_state_in[w.rh * size + j] = 0.0f;
             continue;
         }
-        const float decay = fmaxf(log2_decay(a.log_decay, h), -1e9f);  // (all at once, and none of no ticks)
-        // a lane's elements of a state, as offsets from a place that is the same for all; worked out where they are needed
-        // and not kept meanwhile
-        const auto each = [&](int along_keys, int along_values, auto visit) {
-            int here = 0;
-            asm volatile("" : "+v"(here));
-            const int value = 16 * wave + (lane & 15) + here, first_key = 4 * (lane >> 4) + here, at = first_key * along_keys + value * along_values;
-            if (a.keys == D && a.values == D) {
-#pragma unroll
-                for (int s = 0; s < A::TILES; ++s)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) visit(s, i, (16 * s + i) * along_keys, at);
-            } else if (value < a.values) {
-#pragma unroll
-                for (int s = 0; s < A::TILES; ++s)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (first_key + 16 * s + i < a.keys) visit(s, i, (16 * s + i) * along_keys, at);
-            }
-        };
-        typename A::State state;
-#pragma unroll
-        for (int s = 0; s < A::TILES; ++s) state[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        if (!CARRY && a.carried) {
-            const float *const from = a.carried + w * a.keys * a.values;
-            each(a.values, 1, [&](int s, int i, int from_there, int at) { state[s][i] = (from + from_there)[at]; });
-        } else if (!CARRY && a.state_in) {
-            const float *const from = a.state_in + rh * a.keys * a.values;
-            each((int)a.state_key, (int)a.state_value, [&](int s, int i, int from_there, int at) { state[s][i] = (from + from_there)[at]; });
+        const typename A::Decay decay(a.log_decay, w.h);
+        const uint8_t *const fresh = a.fresh ? a.fresh + w.env : nullptr;
+        const void *const qa = moved_on(a.q, w.of(a.qs), bytes), *const ka = moved_on(a.k, w.of(a.ks), bytes),
+                          *const va = moved_on(a.v, w.of(a.vs), bytes), *const ga = moved_on(a.grad_out, w.of(a.os), bytes);
+        if (a.grad_q) {
+            const Part part = {ga, va, ka, gq, a.os.tick, a.vs.tick, a.ks.tick, a.gqs.tick, a.values, a.keys, 0, a.scale, 1.0f};
+            typename A::State state;               // transposed
+            if (a.states) A::load_state(state, a.states + w.at * size, a.values, a.keys, 1, a.values);
+            else if (a.state_in) A::load_state(state, a.state_in + w.rh * size, a.values, a.keys, 1, a.values);
+            else A::clear(state);
+            float kept = 1.0f;
+            A::template go_through<true>(state, kept, g, v, k, within[0], wild, turn, part, Course{fresh, a.envs, a.ticks, first, 0}, last, decay);
         }
-        float power[4];                            // of the decay, for 0 to 3 ticks
-#pragma unroll
-        for (int i = 0; i < 4; ++i) power[i] = __builtin_amdgcn_exp2f(decay * (float)i);
-        float kept = 1.0f;
-        typename A::Rows qr, kr, vr;
+        if (!a.grad_k && !a.grad_v && !a.grad_state_in) continue;
+        const Part to_k = {va, ga, qa, a.grad_k ? gk : nullptr, a.vs.tick, a.os.tick, a.qs.tick, a.gks.tick, a.values, a.keys, 1, 1.0f, a.scale};
+        const Part to_v = {ka, qa, ga, a.grad_v ? gv : nullptr, a.ks.tick, a.qs.tick, a.os.tick, a.gvs.tick, a.keys, a.values, 1, 1.0f, a.scale};
+        // the segment that ends where the one forwards begins to count
+        const int segment = a.segments - 1 - w.segment;
+        const int64_t from = segment * a.segment, to = min(from + a.segment, a.ticks);
+        typename A::State turned, state;
+        if (a.grad_states) {
+            const float *const s = a.grad_states + (w.rh * a.segments + segment) * size;
+            A::load_state(turned, s, a.values, a.keys, 1, a.values);
+            A::load_state(state, s, a.keys, a.values, a.values, 1);
+        } else if (a.grad_state_out) {
+            A::load_state(turned, a.grad_state_out + w.rh * size, a.values, a.keys, 1, a.values);
+            A::load_state(state, a.grad_state_out + w.rh * size, a.keys, a.values, a.values, 1);
+        } else {
+            A::clear(turned);
+            A::clear(state);
+        }
+        Course next = {fresh, a.envs, a.ticks, from, 1};
+        typename A::Rows qr, kr, vr, gr;
         int flag = 0;
-        Course next = {a.ticks, first, a.backward};
         const auto fetch = [&](int n) {
-            if constexpr (!CARRY) A::load(qr, a.q, q_at, a.qs.tick, next, n, a.keys);
-            A::load(kr, a.k, k_at, a.ks.tick, next, n, a.keys);
-            A::load(vr, a.v, v_at, a.vs.tick, next, n, a.values);
-            flag = 0;
-            if (a.fresh && lane < n) {
-                // backwards, an episode begins behind the tick where, forwards, the next one does
-                const int64_t t = next.begin + lane;
-                if (!a.backward) flag = a.fresh[t * a.envs + env];
-                else if (t > 0) flag = a.fresh[(a.ticks - t) * a.envs + env];
-            }
+            A::load(qr, qa, a.qs.tick, next, n, a.keys);
+            A::load(kr, ka, a.ks.tick, next, n, a.keys);
+            A::load(vr, va, a.vs.tick, next, n, a.values);
+            A::load(gr, ga, a.os.tick, next, n, a.values);
+            flag = next.begins(lane, n);
         };
-        if (first < last) fetch((int)min((int64_t)C, last - first));
-        for (int64_t begin = first; begin < last; begin += C) {
-            const int n = (int)min((int64_t)C, last - begin);
+        if (from < to) fetch((int)min((int64_t)C, to - from));
+        while (next.begin < to) {
+            const int n = (int)min((int64_t)C, to - next.begin);
             const Course here = next;
-            // powers and places are worked out for every chunk: kept, they would cost a wavefront
-            float l2 = decay;
+            float l2 = decay.l2;                   // (as in go_through)
             int col = lane & 15, quad = lane >> 4;
             asm volatile("" : "+v"(l2), "+v"(col), "+v"(quad));
             turn ^= 1;
             if (threadIdx.x == 0) wild[turn] = 0;
-            __syncthreads();                                   // the chunk before has been worked on
-            if constexpr (!CARRY) A::store(q, qr);
-            const uint32_t odd = A::store(k, kr) | A::store(v, vr);
-            if (__ballot(odd != 0) && lane == 0) wild[turn] = 1;
-            const uint64_t begins = __ballot(flag != 0);       // bit i: an episode begins with the chunk's tick i
-            next.begin += C;
-            if (next.begin < last) fetch((int)min((int64_t)C, last - next.begin));
             __syncthreads();
-            if constexpr (!CARRY) {
-                A::compare(within, q, k, begins, l2, power, a.scale_within, wave, col, quad);
-                __syncthreads();
+            A::store(k, kr);
+            A::store(v, vr);
+            const uint32_t odd = A::store(q, qr) | A::store(g, gr);
+            if (__ballot(odd != 0) && lane == 0) wild[turn] = 1;
+            const uint64_t begins = __ballot(flag != 0);
+            next.begin += C;
+            if (next.begin < to) fetch((int)min((int64_t)C, to - next.begin));
+            __syncthreads();
+            if (a.grad_k) A::compare(within[0], v, g, begins, l2, decay.power, a.scale, wave, col, quad);
+            if (a.grad_v) A::compare(within[1], k, q, begins, l2, decay.power, a.scale, wave, col, quad);
+            __syncthreads();
+            if (__builtin_expect(wild[turn], 0)) {
+                if (a.grad_k) A::template advance_slowly<true>(turned, begins, n, l2, to_k, here, wave, col, quad);
+                A::template advance_slowly<true>(state, begins, n, l2, to_v, here, wave, col, quad);
+            } else {
+                if (a.grad_k) A::template advance<true>(turned, within[0], v, g, q, begins, n, l2, decay.power, to_k, here, wave, col, quad);
+                A::template advance<true>(state, within[1], k, q, g, begins, n, l2, decay.power, to_v, here, wave, col, quad);
             }
-            if (__builtin_expect(wild[turn], 0)) A::template advance_slowly<!CARRY>(state, begins, n, l2, a, here, q_at, k_at, v_at, out_at, wave, col, quad);
-            else A::template advance<!CARRY>(state, within, q, k, v, begins, n, l2, power, a, here, out_at, wave, col, quad);
-            kept = begins || kept < 0.0f ? -1.0f : kept * __builtin_amdgcn_exp2f(l2 * (float)n);
         }
-        float *const to = CARRY ? a.carried + w * a.keys * a.values : segment == a.segments - 1 ? a.state_out : nullptr;
-        if (CARRY && threadIdx.x == 0) a.kept[w] = kept;
-        if (!to) continue;
-        // backwards, what is left for the state before the first tick, if that belongs to its episode
-        const bool cut = !CARRY && a.backward && a.fresh && a.ticks > 0 && a.fresh[env] != 0;
-        if (CARRY) {
-            each(a.values, 1, [&](int s, int i, int from_there, int at) { (to + from_there)[at] = state[s][i]; });
-        } else {
-            float *const of = to + rh * a.keys * a.values;
-            each((int)a.state_key, (int)a.state_value, [&](int s, int i, int from_there, int at) { (of + from_there)[at] = cut ? 0.0f : state[s][i]; });
-        }
+        // what is left for the state before the first tick, if that belongs to its episode
+        if (a.grad_state_in && segment == a.segments - 1)
+            A::store_state(state, a.grad_state_in + w.rh * size, a.keys, a.values, a.values, 1, fresh && a.ticks > 0 && fresh[0] != 0);
     }
 }
 
@@ -676,7 +853,7 @@ static __global__ __launch_bounds__(256) void tabx_attention_join_kernel(const A
     for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < all; at += (int64_t)gridDim.x * 256) {
         const int64_t rh = at / size, d = at % size;
         if (a.controlled && a.controlled[rh / a.heads] == 0) continue;
-        float s = a.state_in ? a.state_in[rh * size + d / a.values * a.state_key + d % a.values * a.state_value] : 0.0f;
+        float s = a.state_in ? a.state_in[rh * size + d] : 0.0f;
         float *const of = a.carried + rh * a.segments * size + d;
         const float *const kept = a.kept + rh * a.segments;
         for (int n = 0; n < a.segments; n += AHEAD) {          // (what the last one leaves is the attention's to work out)

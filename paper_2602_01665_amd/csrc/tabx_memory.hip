@@ -205,65 +205,77 @@ static int check_attention(int64_t ticks, int64_t rows, int32_t heads, int32_t k
     return TABX_OK;
 }
 
-// Into how many segments of how many ticks a row's ticks are cut: where there are few rows and heads, so many that
-// the machine has something to do, each of several chunks.
+// Keys and values as wide as the kernels' forms take them.
+static int form_width(int32_t keys, int32_t values)
+{
+    const int width = keys > values ? keys : values;
+    return width <= 32 ? 32 : width <= 64 ? 64 : 128;
+}
+
+// Into how many segments of how many ticks a row's ticks are cut: where there are few rows and heads, so many that every
+// CU has the workgroups that it holds, each of some chunks.
 struct Segments {
     int64_t count, ticks;
 };
 constexpr int64_t kSegmentTicks = 128;             // at least; a multiple of every chunk
-constexpr int64_t kSegmentWorks = 1024;            // of the whole call, about
 
-static Segments segments_of(int64_t ticks, int64_t rows, int32_t heads)
+static Segments segments_of(int64_t ticks, int64_t rows, int32_t heads, int32_t keys, int32_t values)
 {
-    const int64_t works = rows * heads;
-    int64_t most = works > 0 ? kSegmentWorks / works : 1;
-    if (most < 1) most = 1;
+    const int64_t works = rows * heads, wanted = kComputeUnits * (128 / form_width(keys, values));
+    const int64_t most = works > 0 && works < wanted ? wanted / works : 1;
     int64_t length = quotient_up(quotient_up(ticks, most), kSegmentTicks) * kSegmentTicks;
     if (length < kSegmentTicks) length = kSegmentTicks;
     const int64_t count = quotient_up(ticks, length);
     return Segments{count < 1 ? 1 : count, length};
 }
 
+// Of the states before each segment, and behind them what each leaves of the one before: once for the way forth, twice for
+// the way back.
+static int64_t carried_bytes(const Segments &s, int64_t rows, int32_t heads, int32_t keys, int32_t values)
+{
+    return s.count == 1 ? 0 : quotient_up(rows * heads * s.count * ((int64_t)keys * values + 1) * (int64_t)sizeof(float), 16) * 16;
+}
+
 static int64_t attention_workspace(int64_t ticks, int64_t rows, int32_t heads, int32_t keys, int32_t values)
 {
-    const Segments s = segments_of(ticks, rows, heads);
-    return s.count == 1 ? 0 : rows * heads * s.count * ((int64_t)keys * values + 1) * (int64_t)sizeof(float);
+    return 2 * carried_bytes(segments_of(ticks, rows, heads, keys, values), rows, heads, keys, values);
 }
 
 template <bool CARRY, int D>
-static int launch_attention(const AttentionArgs &a, void *stream)
+static int launch_attention(const AttentionArgs &a, int type, void *stream)
 {
-    return launch(a.type == TABX_F32    ? tabx_attention_kernel<D, TABX_F32, CARRY>
-                  : a.type == TABX_BF16 ? tabx_attention_kernel<D, TABX_BF16, CARRY>
-                                        : tabx_attention_kernel<D, TABX_F16, CARRY>,
+    return launch(type == TABX_F32    ? tabx_attention_kernel<D, TABX_F32, CARRY>
+                  : type == TABX_BF16 ? tabx_attention_kernel<D, TABX_BF16, CARRY>
+                                      : tabx_attention_kernel<D, TABX_F16, CARRY>,
                   least(a.works, kMostGroups), 4 * D, a, stream);
 }
 
 template <bool CARRY>
-static int attention_of_width(const AttentionArgs &a, void *stream)
+static int attention_of_width(const AttentionArgs &a, int type, void *stream)
 {
-    const int width = a.keys > a.values ? a.keys : a.values;
-    if (width <= 32) return launch_attention<CARRY, 32>(a, stream);
-    if (width <= 64) return launch_attention<CARRY, 64>(a, stream);
-    return launch_attention<CARRY, 128>(a, stream);
+    const int width = form_width(a.keys, a.values);
+    return width == 32 ? launch_attention<CARRY, 32>(a, type, stream) : width == 64 ? launch_attention<CARRY, 64>(a, type, stream)
+                                                                                    : launch_attention<CARRY, 128>(a, type, stream);
 }
 
-static int attention(AttentionArgs a, void *workspace, void *stream)
+// The states before each segment, into the workspace.
+static int carry(AttentionArgs &a, int type, void *workspace, void *stream)
 {
-    const Segments s = segments_of(a.ticks, a.rows, a.heads);
-    a.segments = (int32_t)s.count;
-    a.segment = s.ticks;
-    a.works = a.rows * a.heads * s.count;
-    a.envs = a.rows / a.units;
-    if (s.count > 1) {
-        a.carried = (float *)workspace;
-        a.kept = a.carried + a.works * a.keys * a.values;
-        int rc = attention_of_width<true>(a, stream);
-        if (rc) return rc;
-        const int64_t states = a.rows * a.heads * a.keys * a.values;
-        if ((rc = launch(tabx_attention_join_kernel, least(quotient_up(states, 256), kMostGroups), 256, a, stream))) return rc;
-    }
-    return attention_of_width<false>(a, stream);
+    a.carried = (float *)workspace;
+    a.kept = a.carried + a.works * a.keys * a.values;
+    const int rc = attention_of_width<true>(a, type, stream);
+    if (rc) return rc;
+    const int64_t states = a.rows * a.heads * a.keys * a.values;
+    return launch(tabx_attention_join_kernel, least(quotient_up(states, 256), kMostGroups), 256, a, stream);
+}
+
+template <int D>
+static int launch_attention_grad(const AttentionGradArgs &a, int type, void *stream)
+{
+    return launch(type == TABX_F32    ? tabx_attention_grad_kernel<D, TABX_F32>
+                  : type == TABX_BF16 ? tabx_attention_grad_kernel<D, TABX_BF16>
+                                      : tabx_attention_grad_kernel<D, TABX_F16>,
+                  least(a.works, kMostGroups), 4 * D, a, stream);
 }
 
 template <int TYPE, int VALUES, int LANES>
@@ -443,17 +455,21 @@ int tabx_linear_attention(int64_t ticks, int64_t rows, int32_t heads, int32_t ke
     if (ticks > 0 && (rc = check_inputs(ticks, rows, heads, key_width, value_width, q, k, v, out, true))) return rc;
     if ((rc = check_floats(log_decay, false)) || (rc = check_floats(state_in, true)) || (rc = check_floats(state_out, true))) return rc;
     if ((rc = check_workspace(workspace, workspace_bytes, attention_workspace(ticks, rows, heads, key_width, value_width)))) return rc;
+    const Segments s = segments_of(ticks, rows, heads, key_width, value_width);
     AttentionArgs a = {};
+    int type = TABX_F32;
     if (ticks > 0) {
         a.q = q->data, a.k = k->data, a.v = v->data, a.out = out->data;
         a.qs = strides_of(*q), a.ks = strides_of(*k), a.vs = strides_of(*v), a.os = strides_of(*out);
-        a.type = q->type;
+        type = q->type;
     }
     a.log_decay = log_decay, a.fresh = fresh, a.controlled = controlled;
-    a.state_in = state_in, a.state_out = state_out, a.state_key = value_width, a.state_value = 1;
-    a.ticks = ticks, a.rows = rows, a.heads = heads, a.units = units, a.keys = key_width, a.values = value_width;
-    a.scale_within = a.scale_state = scale, a.scale_added = 1.0f;
-    return attention(a, workspace, stream);
+    a.state_in = state_in, a.state_out = state_out;
+    a.ticks = ticks, a.rows = rows, a.envs = rows / units, a.works = rows * heads * s.count, a.segment = s.ticks;
+    a.segments = (int32_t)s.count, a.heads = heads, a.units = units, a.keys = key_width, a.values = value_width;
+    a.scale_read = scale, a.scale_added = 1.0f;
+    if (s.count > 1 && (rc = carry(a, type, workspace, stream))) return rc;
+    return attention_of_width<false>(a, type, stream);
 }
 
 int tabx_linear_attention_backward(int64_t ticks, int64_t rows, int32_t heads, int32_t key_width, int32_t value_width,
@@ -482,44 +498,43 @@ int tabx_linear_attention_backward(int64_t ticks, int64_t rows, int32_t heads, i
         (rc = check_floats(grad_state_in, true)))
         return rc;
     if ((rc = check_workspace(workspace, workspace_bytes, attention_workspace(ticks, rows, heads, key_width, value_width)))) return rc;
-    AttentionArgs b = {};
-    b.log_decay = log_decay, b.fresh = fresh, b.controlled = controlled;
-    b.ticks = ticks, b.rows = rows, b.heads = heads, b.units = units;
-    b.zero_out = 1;
-    if (ticks > 0) b.type = q->type;
-    const auto with = [&](AttentionArgs &a, const TabxHeads *x, const TabxHeads *y, const TabxHeads *z, const TabxHeads *out, int32_t keys,
-                          int32_t values) {
-        a.keys = keys, a.values = values;
-        if (ticks > 0) {
-            a.q = x->data, a.k = y->data, a.v = z->data;
-            a.qs = strides_of(*x), a.ks = strides_of(*y), a.vs = strides_of(*z);
-            if (out) a.out = out->data, a.os = strides_of(*out);
+    const Segments s = segments_of(ticks, rows, heads, key_width, value_width);
+    AttentionGradArgs a = {};
+    int type = TABX_F32;
+    if (ticks > 0) {
+        a.q = q->data, a.k = k->data, a.v = v->data, a.grad_out = grad_out->data;
+        a.qs = strides_of(*q), a.ks = strides_of(*k), a.vs = strides_of(*v), a.os = strides_of(*grad_out);
+        if (grad_q) a.grad_q = grad_q->data, a.gqs = strides_of(*grad_q);
+        if (grad_k) a.grad_k = grad_k->data, a.gks = strides_of(*grad_k);
+        if (grad_v) a.grad_v = grad_v->data, a.gvs = strides_of(*grad_v);
+        type = q->type;
+    }
+    a.log_decay = log_decay, a.fresh = fresh, a.controlled = controlled;
+    a.state_in = state_in, a.grad_state_out = grad_state_out, a.grad_state_in = grad_state_in;
+    a.ticks = ticks, a.rows = rows, a.envs = rows / units, a.works = rows * heads * s.count, a.segment = s.ticks;
+    a.segments = (int32_t)s.count, a.heads = heads, a.units = units, a.keys = key_width, a.values = value_width;
+    a.scale = scale;
+    if (s.count > 1) {
+        AttentionArgs c = {};
+        c.log_decay = log_decay, c.fresh = fresh, c.controlled = controlled;
+        c.ticks = a.ticks, c.rows = a.rows, c.envs = a.envs, c.works = a.works, c.segment = a.segment;
+        c.segments = a.segments, c.heads = heads, c.units = units, c.keys = key_width, c.values = value_width;
+        if (grad_q) {
+            c.k = a.k, c.v = a.v, c.ks = a.ks, c.vs = a.vs;
+            c.state_in = state_in, c.scale_added = 1.0f;
+            if ((rc = carry(c, type, workspace, stream))) return rc;
+            a.states = c.carried;
         }
-    };
-    if (ticks > 0 && grad_q) {                     // values are the keys, and the state lies transposed
-        AttentionArgs a = b;
-        with(a, grad_out, v, k, grad_q, value_width, key_width);
-        a.state_in = state_in, a.state_key = 1, a.state_value = value_width;
-        a.scale_within = a.scale_state = scale, a.scale_added = 1.0f;
-        if ((rc = attention(a, workspace, stream))) return rc;
+        if (grad_k || grad_v || grad_state_in) {
+            c.k = a.q, c.v = a.grad_out, c.ks = a.qs, c.vs = a.os;
+            c.state_in = grad_state_out, c.scale_added = scale, c.backward = 1;
+            if ((rc = carry(c, type, (char *)workspace + carried_bytes(s, rows, heads, key_width, value_width), stream))) return rc;
+            a.grad_states = c.carried;
+        }
     }
-    b.backward = 1;
-    b.state_in = grad_state_out;
-    b.scale_within = scale, b.scale_state = 1.0f, b.scale_added = scale;
-    if (ticks > 0 && grad_k) {
-        AttentionArgs a = b;
-        with(a, v, grad_out, q, grad_k, value_width, key_width);
-        a.state_key = 1, a.state_value = value_width;
-        if ((rc = attention(a, workspace, stream))) return rc;
-    }
-    if (grad_v || grad_state_in) {
-        AttentionArgs a = b;
-        with(a, k, q, grad_out, grad_v, key_width, value_width);
-        a.state_key = value_width, a.state_value = 1;
-        a.state_out = grad_state_in;
-        if ((rc = attention(a, workspace, stream))) return rc;
-    }
-    return TABX_OK;
+    const int width = form_width(key_width, value_width);
+    return width == 32 ? launch_attention_grad<32>(a, type, stream) : width == 64 ? launch_attention_grad<64>(a, type, stream)
+                                                                                  : launch_attention_grad<128>(a, type, stream);
 }
 
 } // extern "C"
