@@ -223,12 +223,12 @@ struct Eight {
         for (int n = 0; n < PIECES; ++n) v[n] = u32x4{0, 0, 0, 0};
         if (count >= 8) {
             load(from);
-        } else if (count > 0) {                    // a width that is no multiple of eight
+        } else if (count > 0) {                    // a width that is no multiple of eight: the last element for those behind it
 #pragma unroll
             for (int i = 0; i < 7; ++i) {
-                if (i >= count) continue;
-                if constexpr (TYPE == TABX_F32) v[i / 4][i % 4] = ((const uint32_t *)from)[i];
-                else v[0][i / 2] |= (uint32_t)((const uint16_t *)from)[i] << 16 * (i % 2);
+                const int at = min(i, count - 1);
+                if constexpr (TYPE == TABX_F32) v[i / 4][i % 4] = i < count ? ((const uint32_t *)from)[at] : 0;
+                else v[0][i / 2] |= i < count ? (uint32_t)((const uint16_t *)from)[at] << 16 * (i % 2) : 0;
             }
         }
     }
@@ -340,11 +340,17 @@ __device__ __forceinline__ T *moved_on(T *data, int64_t elements, int bytes)
 template <int D, int TYPE>
 struct Attention {
     static constexpr int C = chunk_of(D, TYPE), IN = Parts<TYPE>::in, MID = Parts<TYPE>::mid;
+    static constexpr bool kAhead = D < 96;
     static constexpr int WAVES = D / 16, THREADS = 64 * WAVES, PASSES = C * D / 8 / THREADS, TILES = D / 16;
     typedef typename Element<TYPE>::one T;
     typedef Tile<D, C, IN> In;
-    static constexpr int kWithin = C + 8;          // distance of rows of the products of queries and keys
-    typedef __bf16 Within[MID][C * kWithin];
+    // Products of queries and keys: rows of the first 32 queries have the first 32 keys only.
+    static constexpr int kNear = 32 + 8, kFar = 64 + 8;
+    typedef __bf16 Within[MID][C == 64 ? 32 * kNear + 32 * kFar : 32 * kNear];
+    static __device__ __forceinline__ int within_row(int I, int col)
+    {
+        return I < 2 ? (16 * I + col) * kNear : 32 * kNear + (16 * (I - 2) + col) * kFar;
+    }
 
     // A wavefront has 16 of the values and all of the state's lines of them, in the layout in which a product leaves its
     // result (a lane has four lines of one column), which is that of an operand of the next one (`along_results`).
@@ -356,6 +362,7 @@ struct Attention {
     {
         constexpr int across = D / 8;
         const int d = 8 * ((int)threadIdx.x % across), row = (int)threadIdx.x / across;
+        asm volatile("" : "+s"(tick));             // (what follows from it is not kept)
         const int64_t step = c.backward ? -tick : tick;
         const T *const from = (const T *)data + c.tick(0) * tick + row * step + d;
         if (n == C && width == D) {                // (the same for all: no lane has to be asked)
@@ -384,9 +391,10 @@ struct Attention {
     // Products of queries and keys, faded by the ticks between them, 0 where they do not belong together, in parts:
     // tiles of 16 x 16 on and below the diagonal, dealt to the wavefronts.  Rows are queries; along them the keys lie in the
     // order of `along_results`, so that a lane's eight are next to each other.
-    static __device__ __forceinline__ void compare(Within &within, const In &q, const In &k, uint64_t begins, float l2, const float (&power)[4],
-                                                   float scale, int wave, int col, int quad)
+    static __device__ __forceinline__ void compare(Within &within, const In &q, const In &k, uint64_t begins, float l2, float scale, int wave, int col,
+                                                   int quad)
     {
+        const Powers power(l2);
         constexpr int tiles = C / 16 * (C / 16 + 1) / 2;
         for (int tile = wave; tile < tiles; tile += WAVES) {
             const int I = tile < 1 ? 0 : tile < 3 ? 1 : tile < 6 ? 2 : 3, J = tile - I * (I + 1) / 2;
@@ -402,7 +410,7 @@ struct Attention {
             if (I > J) {
                 const float fade = __builtin_amdgcn_exp2f(l2 * (float)(i - first - 3)) * scale;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) p[r] *= fade * power[3 - r];
+                for (int r = 0; r < 4; ++r) p[r] *= fade * power.of[3 - r];
             } else {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) p[r] = first + r <= i ? p[r] * (__builtin_amdgcn_exp2f(l2 * (float)(i - first - r)) * scale) : 0.0f;
@@ -415,7 +423,7 @@ struct Attention {
             }
             bf16x4 part[MID];
             split(part, p);
-            const int at = i * kWithin + 32 * (J / 2) + 8 * quad + 4 * (J % 2);
+            const int at = within_row(I, col) + 32 * (J / 2) + 8 * quad + 4 * (J % 2);
 #pragma unroll
             for (int m = 0; m < MID; ++m) {
                 *(bf16x4 *)&within[m][at] = part[m];
@@ -427,8 +435,8 @@ struct Attention {
     // What a chunk's queries read, and the state behind the chunk.
     template <bool READS>
     static __device__ __forceinline__ void advance(State &state, const Within &within, const In &q, const In &k, const In &v,
-                                                   uint64_t begins, int n, float l2, const float (&power)[4], const Part &a, const Course &c,
-                                                   int wave, int col, int quad)
+                                                   uint64_t begins, int n, float l2, const Part &a, const Course &c, int wave, int col,
+                                                   int quad)
     {
         bf16x8 values[C / 32][IN];                 // this lane's: 8 ticks of its column, of every 32
 #pragma unroll
@@ -444,8 +452,10 @@ struct Attention {
                 for (int m = 0; m < MID; ++m) held[s][m] = join(x[m], y[m]);
             }
             const int d = 16 * wave + 4 * quad;
-            const int64_t step = c.backward ? -a.out_tick : a.out_tick;
-            T *const out = (T *)a.out + c.tick(0) * a.out_tick + col * step + d;
+            int64_t tick = a.out_tick;
+            asm volatile("" : "+s"(tick));
+            const int64_t step = c.backward ? -tick : tick;
+            T *const out = (T *)a.out + c.tick(0) * tick + col * step + d;
 #pragma unroll
             for (int I = 0; I < C / 16; ++I) {
                 if (16 * I >= n) continue;
@@ -469,7 +479,7 @@ struct Attention {
                 for (int b = 0; b <= I / 2; ++b) {
                     bf16x8 x[MID];
 #pragma unroll
-                    for (int m = 0; m < MID; ++m) x[m] = *(const bf16x8 *)&within[m][i * kWithin + 32 * b + 8 * quad];
+                    for (int m = 0; m < MID; ++m) x[m] = *(const bf16x8 *)&within[m][within_row(I, col) + 32 * b + 8 * quad];
                     o = multiply(values[b], x, o);
                 }
                 if (a.out && i < n && d < a.values) {
@@ -488,24 +498,25 @@ struct Attention {
         // the values faded by the ticks behind theirs; those of episodes that have ended count no more
         const int newest = begins ? 63 - __builtin_clzll(begins) : 0;
         const float left = __builtin_amdgcn_exp2f(l2 * (float)n);
+        const Powers power(l2);
         bf16x8 faded[C / 32][MID];
 #pragma unroll
         for (int b = 0; b < C / 32; ++b) {
             bf16x4 part[2][MID];
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+                f32x4 x;
 #pragma unroll
                 for (int p = IN - 1; p >= 0; --p) {
                     const bf16x4 y = half ? __builtin_shufflevector(values[b][p], values[b][p], 4, 5, 6, 7)
                                           : __builtin_shufflevector(values[b][p], values[b][p], 0, 1, 2, 3);
-                    x += __builtin_convertvector(y, f32x4);
+                    x = p == IN - 1 ? __builtin_convertvector(y, f32x4) : x + __builtin_convertvector(y, f32x4);
                 }
                 const int first = 32 * b + 16 * half + 4 * quad;
                 if (n == C) {
                     const float fade = __builtin_amdgcn_exp2f(l2 * (float)(C - 4 - first + a.backward)) * a.scale_added;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) x[r] *= fade * power[3 - r];
+                    for (int r = 0; r < 4; ++r) x[r] *= fade * power.of[3 - r];
                 } else {
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
@@ -615,38 +626,43 @@ struct Attention {
         for (int s = 0; s < TILES; ++s) state[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
-    struct Decay {
-        float l2, power[4];        // its logarithm, and what it leaves in 0 to 3 ticks
-        __device__ __forceinline__ Decay(const float *log_decay, int h)
+    // What the decay leaves in 0 to 3 ticks.
+    struct Powers {
+        float of[4];
+        __device__ __forceinline__ Powers(float l2)
         {
-            l2 = fmaxf(log2_decay(log_decay, h), -1e9f);       // (all at once, and none of no ticks)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) power[i] = __builtin_amdgcn_exp2f(l2 * (float)i);
+            for (int i = 0; i < 4; ++i) of[i] = __builtin_amdgcn_exp2f(l2 * (float)i);
         }
     };
 
-    // One attention from tick `first` to `last`; the next chunk's rows are under way while it works on the present one.
-    // READS: queries are answered (else only the state goes on).  kept: what is left of the state before.  wild, turn: of the
-    // chunk at hand and the one before, whether not all of it is finite.
-    template <bool READS>
+    // One attention from tick `begin` to `last`; the next chunk's rows are under way while it works on the present one (not
+    // the wide ones', whose registers cost a workgroup of a CU: 810 us with them, 620 without, 128 ticks of 10240 heads of
+    // 128).  READS: queries are answered (else only the state goes on).  part(), course(begin): what to go through, worked
+    // out anew where it is needed.  kept: what is left of the state before.  wild, turn: of the chunk at hand and the one
+    // before, whether not all of it is finite.
+    template <bool READS, typename GetPart, typename GetCourse>
     static __device__ __forceinline__ void go_through(State &state, float &kept, In &q, In &k, In &v, Within &within, int (&wild)[2], int &turn,
-                                                      const Part &a, Course next, int64_t last, const Decay &decay)
+                                                      GetPart part, GetCourse course, int64_t begin, int64_t last, float decay)
     {
         const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
         Rows qr, kr, vr;
         int flag = 0;
-        const auto fetch = [&](int n) {
-            if constexpr (READS) load(qr, a.q, a.q_tick, next, n, a.keys);
-            load(kr, a.k, a.k_tick, next, n, a.keys);
-            load(vr, a.v, a.v_tick, next, n, a.values);
-            flag = next.begins(lane, n);
+        const auto fetch = [&](int64_t from) {
+            const Part a = part();
+            const Course c = course(from);
+            const int n = (int)min((int64_t)C, last - from);
+            if constexpr (READS) load(qr, a.q, a.q_tick, c, n, a.keys);
+            load(kr, a.k, a.k_tick, c, n, a.keys);
+            load(vr, a.v, a.v_tick, c, n, a.values);
+            flag = c.begins(lane, n);
         };
-        if (next.begin < last) fetch((int)min((int64_t)C, last - next.begin));
-        while (next.begin < last) {
-            const int n = (int)min((int64_t)C, last - next.begin);
-            const Course here = next;
+        if (kAhead && begin < last) fetch(begin);
+        for (; begin < last; begin += C) {
+            const int n = (int)min((int64_t)C, last - begin);
+            if (!kAhead) fetch(begin);
             // powers and places are worked out for every chunk: kept, they would cost a wavefront
-            float l2 = decay.l2;
+            float l2 = decay;
             int col = lane & 15, quad = lane >> 4;
             asm volatile("" : "+v"(l2), "+v"(col), "+v"(quad));
             turn ^= 1;
@@ -656,15 +672,17 @@ struct Attention {
             const uint32_t odd = store(k, kr) | store(v, vr);
             if (__ballot(odd != 0) && lane == 0) wild[turn] = 1;
             const uint64_t begins = __ballot(flag != 0);       // bit i: an episode begins with the chunk's tick i
-            next.begin += C;
-            if (next.begin < last) fetch((int)min((int64_t)C, last - next.begin));
+            if (kAhead && begin + C < last) fetch(begin + C);
             __syncthreads();
             if constexpr (READS) {
-                compare(within, q, k, begins, l2, decay.power, a.scale_read * a.scale_added, wave, col, quad);
+                const Part a = part();
+                compare(within, q, k, begins, l2, a.scale_read * a.scale_added, wave, col, quad);
                 __syncthreads();
             }
-            if (__builtin_expect(wild[turn], 0)) advance_slowly<READS>(state, begins, n, l2, a, here, wave, col, quad);
-            else advance<READS>(state, within, q, k, v, begins, n, l2, decay.power, a, here, wave, col, quad);
+            const Part a = part();
+            const Course c = course(begin);
+            if (__builtin_expect(wild[turn], 0)) advance_slowly<READS>(state, begins, n, l2, a, c, wave, col, quad);
+            else advance<READS>(state, within, q, k, v, begins, n, l2, a, c, wave, col, quad);
             kept = begins || kept < 0.0f ? -1.0f : kept * __builtin_amdgcn_exp2f(l2 * (float)n);
         }
     }
@@ -701,37 +719,61 @@ struct Work {
 };
 
 // Wavefronts of a SIMD, as many as the LDS of a workgroup lets the machine hold.
-constexpr int attention_wavefronts(int d) { return d == 128 ? 2 : 3; }
-constexpr int attention_grad_wavefronts(int d) { return 2; }
+constexpr int attention_wavefronts(int d, int type) { return d >= 96 ? type == TABX_F32 ? 2 : 4 : 3; }
+constexpr int attention_grad_wavefronts(int d, int type) { return d >= 96 ? 2 : type == TABX_F32 ? 2 : 3; }
+
+// The launch arguments, fetched anew for what follows.  A wavefront has too few scalar registers for what all of a kernel
+// needs, and what is fetched once at the top is spilled to vector registers (a quarter of the gradients' instructions).
+template <typename Args>
+__device__ __forceinline__ const Args &again()
+{
+    typedef const __attribute__((address_space(4))) Args *Late;
+    Late p = (Late)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const Args *)p;
+}
 
 // A workgroup goes through its ticks with the state in registers.  CARRY: nothing is read, the states that the segments
 // would leave of nothing are.
 template <int D, int TYPE, bool CARRY>
-__global__ __launch_bounds__(4 * D, attention_wavefronts(D)) void tabx_attention_kernel(const AttentionArgs a)
+__global__ __launch_bounds__(4 * D, attention_wavefronts(D, TYPE)) void tabx_attention_kernel(const AttentionArgs)
 {
     typedef Attention<D, TYPE> A;
+    typedef AttentionArgs Args;
     __shared__ typename A::In q, k, v;
     __shared__ typename A::Within within;
     __shared__ int wild[2];
     int turn = 0;
-    for (int64_t id = blockIdx.x; id < a.works; id += gridDim.x) {
-        const Work w(a, id);
-        if (CARRY && w.segment == a.segments - 1) continue;    // (nothing comes behind it)
-        if (a.controlled && a.controlled[w.r] == 0) continue;
-        constexpr int bytes = sizeof(typename A::T);
-        const Part part = {moved_on(a.q, w.of(a.qs), bytes), moved_on(a.k, w.of(a.ks), bytes), moved_on(a.v, w.of(a.vs), bytes),
-                           moved_on(a.out, w.of(a.os), bytes), a.qs.tick, a.ks.tick, a.vs.tick, a.os.tick, a.keys, a.values, a.backward,
-                           a.scale_read, a.scale_added};
-        const typename A::Decay decay(a.log_decay, w.h);
-        const int64_t size = a.keys * a.values;
+    for (int64_t id = blockIdx.x; id < again<Args>().works; id += gridDim.x) {
+        const Work w(again<Args>(), id);
+        const auto part = [&] {
+            const Args &a = again<Args>();
+            constexpr int bytes = sizeof(typename A::T);
+            return Part{moved_on(a.q, w.of(a.qs), bytes), moved_on(a.k, w.of(a.ks), bytes), moved_on(a.v, w.of(a.vs), bytes),
+                        a.out ? moved_on(a.out, w.of(a.os), bytes) : nullptr, a.qs.tick, a.ks.tick, a.vs.tick, a.os.tick, a.keys, a.values,
+                        a.backward, a.scale_read, a.scale_added};
+        };
+        const auto course = [&](int64_t begin) {
+            const Args &a = again<Args>();
+            return Course{a.fresh ? a.fresh + w.env : nullptr, a.envs, a.ticks, begin, a.backward};
+        };
         typename A::State state;
-        if (!CARRY && a.carried) A::load_state(state, a.carried + w.at * size, a.keys, a.values, a.values, 1);
-        else if (!CARRY && a.state_in) A::load_state(state, a.state_in + w.rh * size, a.keys, a.values, a.values, 1);
-        else A::clear(state);
-        float kept = 1.0f;
-        const int64_t first = w.segment * a.segment;
-        A::template go_through<!CARRY>(state, kept, q, k, v, within, wild, turn, part,
-                                       Course{a.fresh ? a.fresh + w.env : nullptr, a.envs, a.ticks, first, a.backward}, min(first + a.segment, a.ticks), decay);
+        float kept = 1.0f, decay;
+        int64_t first, last;
+        {
+            const Args &a = again<Args>();
+            if (CARRY && w.segment == a.segments - 1) continue;        // (nothing comes behind it)
+            if (a.controlled && a.controlled[w.r] == 0) continue;
+            decay = fmaxf(log2_decay(a.log_decay, w.h), -1e9f);        // (all at once, and none of no ticks)
+            const int64_t size = a.keys * a.values;
+            if (!CARRY && a.carried) A::load_state(state, a.carried + w.at * size, a.keys, a.values, a.values, 1);
+            else if (!CARRY && a.state_in) A::load_state(state, a.state_in + w.rh * size, a.keys, a.values, a.values, 1);
+            else A::clear(state);
+            first = w.segment * a.segment, last = min(first + a.segment, a.ticks);
+        }
+        A::template go_through<!CARRY>(state, kept, q, k, v, within, wild, turn, part, course, first, last, decay);
+        const Args &a = again<Args>();
+        const int64_t size = a.keys * a.values;
         if (CARRY) {
             A::store_state(state, a.carried + w.at * size, a.keys, a.values, a.values, 1, false);
             if (threadIdx.x == 0) a.kept[w.at] = kept;
@@ -744,77 +786,103 @@ __global__ __launch_bounds__(4 * D, attention_wavefronts(D)) void tabx_attention
 // The gradients: forwards through the ticks for grad_q, then backwards for grad_k and grad_v, which read the same rows,
 // and the state's; the last chunk forwards is the first one backwards, and what was read is still in the caches.
 template <int D, int TYPE>
-__global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D)) void tabx_attention_grad_kernel(const AttentionGradArgs a)
+__global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tabx_attention_grad_kernel(const AttentionGradArgs)
 {
     typedef Attention<D, TYPE> A;
+    typedef AttentionGradArgs Args;
     typedef typename A::T T;
     constexpr int C = A::C, bytes = sizeof(T);
+    constexpr bool kAhead = false;
     __shared__ typename A::In q, k, v, g;
-    __shared__ typename A::Within within[2];
+    __shared__ typename A::Within within;
     __shared__ int wild[2];
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     int turn = 0;
-    for (int64_t id = blockIdx.x; id < a.works; id += gridDim.x) {
-        const Work w(a, id);
-        const int64_t first = w.segment * a.segment, last = min(first + a.segment, a.ticks), size = a.keys * a.values;
-        T *const gq = (T *)a.grad_q + w.of(a.gqs), *const gk = (T *)a.grad_k + w.of(a.gks), *const gv = (T *)a.grad_v + w.of(a.gvs);
-        if (a.controlled && a.controlled[w.r] == 0) {
-            for (int64_t t = first; t < last; ++t)
-                for (int j = threadIdx.x; j < max(a.keys, a.values); j += A::THREADS) {
-                    if (a.grad_q && j < a.keys) gq[t * a.gqs.tick + j] = (T)0.0f;
-                    if (a.grad_k && j < a.keys) gk[t * a.gks.tick + j] = (T)0.0f;
-                    if (a.grad_v && j < a.values) gv[t * a.gvs.tick + j] = (T)0.0f;
-                }
-            if (a.grad_state_in && w.segment == 0)
-                for (int j = threadIdx.x; j < size; j += A::THREADS) a.grad_state_in[w.rh * size + j] = 0.0f;
-            continue;
+    for (int64_t id = blockIdx.x; id < again<Args>().works; id += gridDim.x) {
+        const Work w(again<Args>(), id);
+        const auto course = [&](int64_t begin, int backward) {
+            const Args &a = again<Args>();
+            return Course{a.fresh ? a.fresh + w.env : nullptr, a.envs, a.ticks, begin, backward};
+        };
+        float decay;
+        {
+            const Args &a = again<Args>();
+            const int64_t first = w.segment * a.segment, last = min(first + a.segment, a.ticks), size = a.keys * a.values;
+            if (a.controlled && a.controlled[w.r] == 0) {
+                T *const gq = (T *)a.grad_q + w.of(a.gqs), *const gk = (T *)a.grad_k + w.of(a.gks), *const gv = (T *)a.grad_v + w.of(a.gvs);
+                for (int64_t t = first; t < last; ++t)
+                    for (int j = threadIdx.x; j < max(a.keys, a.values); j += A::THREADS) {
+                        if (a.grad_q && j < a.keys) gq[t * a.gqs.tick + j] = (T)0.0f;
+                        if (a.grad_k && j < a.keys) gk[t * a.gks.tick + j] = (T)0.0f;
+                        if (a.grad_v && j < a.values) gv[t * a.gvs.tick + j] = (T)0.0f;
+                    }
+                if (a.grad_state_in && w.segment == 0)
+                    for (int j = threadIdx.x; j < size; j += A::THREADS) a.grad_state_in[w.rh * size + j] = 0.0f;
+                continue;
+            }
+            decay = fmaxf(log2_decay(a.log_decay, w.h), -1e9f);
+            if (a.grad_q) {
+                typename A::State state;           // transposed
+                if (a.states) A::load_state(state, a.states + w.at * size, a.values, a.keys, 1, a.values);
+                else if (a.state_in) A::load_state(state, a.state_in + w.rh * size, a.values, a.keys, 1, a.values);
+                else A::clear(state);
+                float kept = 1.0f;
+                const auto part = [&] {
+                    const Args &a = again<Args>();
+                    return Part{moved_on(a.grad_out, w.of(a.os), bytes), moved_on(a.v, w.of(a.vs), bytes), moved_on(a.k, w.of(a.ks), bytes),
+                                moved_on(a.grad_q, w.of(a.gqs), bytes), a.os.tick, a.vs.tick, a.ks.tick, a.gqs.tick, a.values, a.keys, 0, a.scale, 1.0f};
+                };
+                A::template go_through<true>(state, kept, g, v, k, within, wild, turn, part, [&](int64_t begin) { return course(begin, 0); }, first, last, decay);
+            }
         }
-        const typename A::Decay decay(a.log_decay, w.h);
-        const uint8_t *const fresh = a.fresh ? a.fresh + w.env : nullptr;
-        const void *const qa = moved_on(a.q, w.of(a.qs), bytes), *const ka = moved_on(a.k, w.of(a.ks), bytes),
-                          *const va = moved_on(a.v, w.of(a.vs), bytes), *const ga = moved_on(a.grad_out, w.of(a.os), bytes);
-        if (a.grad_q) {
-            const Part part = {ga, va, ka, gq, a.os.tick, a.vs.tick, a.ks.tick, a.gqs.tick, a.values, a.keys, 0, a.scale, 1.0f};
-            typename A::State state;               // transposed
-            if (a.states) A::load_state(state, a.states + w.at * size, a.values, a.keys, 1, a.values);
-            else if (a.state_in) A::load_state(state, a.state_in + w.rh * size, a.values, a.keys, 1, a.values);
-            else A::clear(state);
-            float kept = 1.0f;
-            A::template go_through<true>(state, kept, g, v, k, within[0], wild, turn, part, Course{fresh, a.envs, a.ticks, first, 0}, last, decay);
-        }
-        if (!a.grad_k && !a.grad_v && !a.grad_state_in) continue;
-        const Part to_k = {va, ga, qa, a.grad_k ? gk : nullptr, a.vs.tick, a.os.tick, a.qs.tick, a.gks.tick, a.values, a.keys, 1, 1.0f, a.scale};
-        const Part to_v = {ka, qa, ga, a.grad_v ? gv : nullptr, a.ks.tick, a.qs.tick, a.os.tick, a.gvs.tick, a.keys, a.values, 1, 1.0f, a.scale};
-        // the segment that ends where the one forwards begins to count
-        const int segment = a.segments - 1 - w.segment;
-        const int64_t from = segment * a.segment, to = min(from + a.segment, a.ticks);
         typename A::State turned, state;
-        if (a.grad_states) {
-            const float *const s = a.grad_states + (w.rh * a.segments + segment) * size;
-            A::load_state(turned, s, a.values, a.keys, 1, a.values);
-            A::load_state(state, s, a.keys, a.values, a.values, 1);
-        } else if (a.grad_state_out) {
-            A::load_state(turned, a.grad_state_out + w.rh * size, a.values, a.keys, 1, a.values);
-            A::load_state(state, a.grad_state_out + w.rh * size, a.keys, a.values, a.values, 1);
-        } else {
-            A::clear(turned);
-            A::clear(state);
+        int64_t begin, last;
+        {
+            const Args &a = again<Args>();
+            if (!a.grad_k && !a.grad_v && !a.grad_state_in) continue;
+            // the segment that ends where the one forwards begins to count
+            const int segment = a.segments - 1 - w.segment;
+            const int64_t size = a.keys * a.values;
+            begin = segment * a.segment, last = min(begin + a.segment, a.ticks);
+            const float *const s = a.grad_states ? a.grad_states + (w.rh * a.segments + segment) * size
+                                                 : a.grad_state_out ? a.grad_state_out + w.rh * size : nullptr;
+            if (s) {
+                A::load_state(turned, s, a.values, a.keys, 1, a.values);
+                A::load_state(state, s, a.keys, a.values, a.values, 1);
+            } else {
+                A::clear(turned);
+                A::clear(state);
+            }
         }
-        Course next = {fresh, a.envs, a.ticks, from, 1};
+        const auto to_k = [&] {
+            const Args &a = again<Args>();
+            return Part{moved_on(a.v, w.of(a.vs), bytes), moved_on(a.grad_out, w.of(a.os), bytes), moved_on(a.q, w.of(a.qs), bytes),
+                        moved_on(a.grad_k, w.of(a.gks), bytes), a.vs.tick, a.os.tick, a.qs.tick, a.gks.tick, a.values, a.keys, 1, 1.0f, a.scale};
+        };
+        const auto to_v = [&] {
+            const Args &a = again<Args>();
+            return Part{moved_on(a.k, w.of(a.ks), bytes), moved_on(a.q, w.of(a.qs), bytes), moved_on(a.grad_out, w.of(a.os), bytes),
+                        a.grad_v ? moved_on(a.grad_v, w.of(a.gvs), bytes) : nullptr, a.ks.tick, a.qs.tick, a.os.tick, a.gvs.tick, a.keys, a.values,
+                        1, 1.0f, a.scale};
+        };
         typename A::Rows qr, kr, vr, gr;
         int flag = 0;
-        const auto fetch = [&](int n) {
-            A::load(qr, qa, a.qs.tick, next, n, a.keys);
-            A::load(kr, ka, a.ks.tick, next, n, a.keys);
-            A::load(vr, va, a.vs.tick, next, n, a.values);
-            A::load(gr, ga, a.os.tick, next, n, a.values);
-            flag = next.begins(lane, n);
+        const auto fetch = [&](int64_t from) {
+            const Course c = course(from, 1);
+            const int n = (int)min((int64_t)C, last - from);
+            const Part a = to_v();
+            A::load(qr, a.k, a.k_tick, c, n, a.keys);
+            A::load(kr, a.q, a.q_tick, c, n, a.keys);
+            A::load(gr, a.v, a.v_tick, c, n, a.values);
+            const Part b = to_k();
+            A::load(vr, b.q, b.q_tick, c, n, b.keys);
+            flag = c.begins(lane, n);
         };
-        if (from < to) fetch((int)min((int64_t)C, to - from));
-        while (next.begin < to) {
-            const int n = (int)min((int64_t)C, to - next.begin);
-            const Course here = next;
-            float l2 = decay.l2;                   // (as in go_through)
+        if (kAhead && begin < last) fetch(begin);
+        for (; begin < last; begin += C) {
+            const int n = (int)min((int64_t)C, last - begin);
+            if (!kAhead) fetch(begin);
+            float l2 = decay;                      // (as in go_through)
             int col = lane & 15, quad = lane >> 4;
             asm volatile("" : "+v"(l2), "+v"(col), "+v"(quad));
             turn ^= 1;
@@ -825,23 +893,29 @@ __global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D)) void tabx_atte
             const uint32_t odd = A::store(q, qr) | A::store(g, gr);
             if (__ballot(odd != 0) && lane == 0) wild[turn] = 1;
             const uint64_t begins = __ballot(flag != 0);
-            next.begin += C;
-            if (next.begin < to) fetch((int)min((int64_t)C, to - next.begin));
+            if (kAhead && begin + C < last) fetch(begin + C);
             __syncthreads();
-            if (a.grad_k) A::compare(within[0], v, g, begins, l2, decay.power, a.scale, wave, col, quad);
-            if (a.grad_v) A::compare(within[1], k, q, begins, l2, decay.power, a.scale, wave, col, quad);
-            __syncthreads();
-            if (__builtin_expect(wild[turn], 0)) {
-                if (a.grad_k) A::template advance_slowly<true>(turned, begins, n, l2, to_k, here, wave, col, quad);
-                A::template advance_slowly<true>(state, begins, n, l2, to_v, here, wave, col, quad);
-            } else {
-                if (a.grad_k) A::template advance<true>(turned, within[0], v, g, q, begins, n, l2, decay.power, to_k, here, wave, col, quad);
-                A::template advance<true>(state, within[1], k, q, g, begins, n, l2, decay.power, to_v, here, wave, col, quad);
+            const bool odd_one = wild[turn] != 0;
+            if (again<Args>().grad_k) {
+                A::compare(within, v, g, begins, l2, again<Args>().scale, wave, col, quad);
+                __syncthreads();
+                const Part a = to_k();
+                const Course c = course(begin, 1);
+                if (__builtin_expect(odd_one, 0)) A::template advance_slowly<true>(turned, begins, n, l2, a, c, wave, col, quad);
+                else A::template advance<true>(turned, within, v, g, q, begins, n, l2, a, c, wave, col, quad);
+                __syncthreads();
             }
+            A::compare(within, k, q, begins, l2, again<Args>().scale, wave, col, quad);
+            __syncthreads();
+            const Part a = to_v();
+            const Course c = course(begin, 1);
+            if (__builtin_expect(odd_one, 0)) A::template advance_slowly<true>(state, begins, n, l2, a, c, wave, col, quad);
+            else A::template advance<true>(state, within, k, q, g, begins, n, l2, a, c, wave, col, quad);
         }
         // what is left for the state before the first tick, if that belongs to its episode
-        if (a.grad_state_in && segment == a.segments - 1)
-            A::store_state(state, a.grad_state_in + w.rh * size, a.keys, a.values, a.values, 1, fresh && a.ticks > 0 && fresh[0] != 0);
+        const Args &a = again<Args>();
+        if (a.grad_state_in && w.segment == 0)
+            A::store_state(state, a.grad_state_in + w.rh * (a.keys * a.values), a.keys, a.values, a.values, 1, a.fresh && a.ticks > 0 && a.fresh[w.env] != 0);
     }
 }
 

@@ -209,7 +209,7 @@ static int check_attention(int64_t ticks, int64_t rows, int32_t heads, int32_t k
 static int form_width(int32_t keys, int32_t values)
 {
     const int width = keys > values ? keys : values;
-    return width <= 32 ? 32 : width <= 64 ? 64 : 128;
+    return width <= 32 ? 32 : width <= 64 ? 64 : width <= 96 ? 96 : 128;
 }
 
 // Into how many segments of how many ticks a row's ticks are cut: where there are few rows and heads, so many that every
@@ -221,7 +221,7 @@ constexpr int64_t kSegmentTicks = 128;             // at least; a multiple of ev
 
 static Segments segments_of(int64_t ticks, int64_t rows, int32_t heads, int32_t keys, int32_t values)
 {
-    const int64_t works = rows * heads, wanted = kComputeUnits * (128 / form_width(keys, values));
+    const int64_t works = rows * heads, wanted = kComputeUnits * (256 / form_width(keys, values));
     const int64_t most = works > 0 && works < wanted ? wanted / works : 1;
     int64_t length = quotient_up(quotient_up(ticks, most), kSegmentTicks) * kSegmentTicks;
     if (length < kSegmentTicks) length = kSegmentTicks;
@@ -254,8 +254,10 @@ template <bool CARRY>
 static int attention_of_width(const AttentionArgs &a, int type, void *stream)
 {
     const int width = form_width(a.keys, a.values);
-    return width == 32 ? launch_attention<CARRY, 32>(a, type, stream) : width == 64 ? launch_attention<CARRY, 64>(a, type, stream)
-                                                                                    : launch_attention<CARRY, 128>(a, type, stream);
+    if (width == 32) return launch_attention<CARRY, 32>(a, type, stream);
+    if (width == 64) return launch_attention<CARRY, 64>(a, type, stream);
+    if (width == 96) return launch_attention<CARRY, 96>(a, type, stream);
+    return launch_attention<CARRY, 128>(a, type, stream);
 }
 
 // The states before each segment, into the workspace.
@@ -533,8 +535,10 @@ int tabx_linear_attention_backward(int64_t ticks, int64_t rows, int32_t heads, i
         }
     }
     const int width = form_width(key_width, value_width);
-    return width == 32 ? launch_attention_grad<32>(a, type, stream) : width == 64 ? launch_attention_grad<64>(a, type, stream)
-                                                                                  : launch_attention_grad<128>(a, type, stream);
+    if (width == 32) return launch_attention_grad<32>(a, type, stream);
+    if (width == 64) return launch_attention_grad<64>(a, type, stream);
+    if (width == 96) return launch_attention_grad<96>(a, type, stream);
+    return launch_attention_grad<128>(a, type, stream);
 }
 
 } // extern "C"
