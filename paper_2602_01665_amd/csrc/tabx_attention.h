@@ -248,6 +248,15 @@ __device__ __forceinline__ uint32_t not_finite(const Eight<TYPE> &e)
     return found & (TYPE == TABX_F32 ? 0x80000000u : 0x80008000u);
 }
 
+// All of a workgroup's wavefronts, and what they have written to LDS.  (__syncthreads would wait for loads that are under way
+// and for stores to memory, which nothing here reads.)
+__device__ __forceinline__ void lds_meet()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // A chunk's rows of one array in LDS, a tile for each part.  Rows lie D + 8 elements apart: eight of them, of 16 bytes
 // each, or four of 32, meet all banks once.
 template <int D, int C, int PARTS>
@@ -340,7 +349,7 @@ __device__ __forceinline__ T *moved_on(T *data, int64_t elements, int bytes)
 template <int D, int TYPE>
 struct Attention {
     static constexpr int C = chunk_of(D, TYPE), IN = Parts<TYPE>::in, MID = Parts<TYPE>::mid;
-    static constexpr bool kAhead = D < 96;
+    static constexpr bool kAhead = D < 96 || TYPE == TABX_F32;
     static constexpr int WAVES = D / 16, THREADS = 64 * WAVES, PASSES = C * D / 8 / THREADS, TILES = D / 16;
     typedef typename Element<TYPE>::one T;
     typedef Tile<D, C, IN> In;
@@ -356,7 +365,17 @@ struct Attention {
     // result (a lane has four lines of one column), which is that of an operand of the next one (`along_results`).
     typedef f32x4 State[TILES];
 
-    struct Rows { Eight<TYPE> e[PASSES]; };
+    struct Rows {
+        Eight<TYPE> e[PASSES];
+        // Waits for them here: later, stores that have been issued meanwhile would be waited for too.
+        __device__ __forceinline__ void arrive()
+        {
+#pragma unroll
+            for (int p = 0; p < PASSES; ++p)
+#pragma unroll
+                for (int n = 0; n < Eight<TYPE>::PIECES; ++n) asm volatile("" : "+v"(e[p].v[n]));
+        }
+    };
 
     static __device__ __forceinline__ void load(Rows &rows, const void *data, int64_t tick, const Course &c, int n, int width)
     {
@@ -433,10 +452,10 @@ struct Attention {
     }
 
     // What a chunk's queries read, and the state behind the chunk.
-    template <bool READS>
+    template <bool READS, typename Arrived>
     static __device__ __forceinline__ void advance(State &state, const Within &within, const In &q, const In &k, const In &v,
                                                    uint64_t begins, int n, float l2, const Part &a, const Course &c, int wave, int col,
-                                                   int quad)
+                                                   int quad, Arrived arrived)
     {
         bf16x8 values[C / 32][IN];                 // this lane's: 8 ticks of its column, of every 32
 #pragma unroll
@@ -482,6 +501,7 @@ struct Attention {
                     for (int m = 0; m < MID; ++m) x[m] = *(const bf16x8 *)&within[m][within_row(I, col) + 32 * b + 8 * quad];
                     o = multiply(values[b], x, o);
                 }
+                if (I == 0) arrived();
                 if (a.out && i < n && d < a.values) {
                     T *const to = out + 16 * I * step;
                     if (d + 4 <= a.values) {
@@ -620,6 +640,22 @@ struct Attention {
             for (int i = 0; i < 4; ++i)
                 if ((keys == D) || first + 16 * s + i < keys) (to + (16 * s + i) * along_keys)[at] = zero ? 0.0f : state[s][i];
     }
+    // Zeros for the ticks from `from` to `to`.
+    static __device__ __forceinline__ void clear_rows(void *data, int64_t tick, int64_t from, int64_t to, int width)
+    {
+        constexpr int across = D / 8;
+        const int d = 8 * ((int)threadIdx.x % across);
+        for (int64_t t = from + (int)threadIdx.x / across; t < to; t += THREADS / across) {
+            T *const at = (T *)data + t * tick + d;
+            if (d + 8 <= width) {
+                const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+                store_four<TYPE>(at, zero);
+                store_four<TYPE>(at + 4, zero);
+            } else {
+                for (int i = d; i < width; ++i) at[i - d] = (T)0.0f;
+            }
+        }
+    }
     static __device__ __forceinline__ void clear(State &state)
     {
 #pragma unroll
@@ -667,22 +703,28 @@ struct Attention {
             asm volatile("" : "+v"(l2), "+v"(col), "+v"(quad));
             turn ^= 1;
             if (threadIdx.x == 0) wild[turn] = 0;
-            __syncthreads();                                   // the chunk before has been worked on
+            lds_meet();                                   // the chunk before has been worked on
             if constexpr (READS) store(q, qr);
             const uint32_t odd = store(k, kr) | store(v, vr);
             if (__ballot(odd != 0) && lane == 0) wild[turn] = 1;
             const uint64_t begins = __ballot(flag != 0);       // bit i: an episode begins with the chunk's tick i
             if (kAhead && begin + C < last) fetch(begin + C);
-            __syncthreads();
+            lds_meet();
             if constexpr (READS) {
                 const Part a = part();
                 compare(within, q, k, begins, l2, a.scale_read * a.scale_added, wave, col, quad);
-                __syncthreads();
+                lds_meet();
             }
             const Part a = part();
             const Course c = course(begin);
             if (__builtin_expect(wild[turn], 0)) advance_slowly<READS>(state, begins, n, l2, a, c, wave, col, quad);
-            else advance<READS>(state, within, q, k, v, begins, n, l2, a, c, wave, col, quad);
+            else
+                advance<READS>(state, within, q, k, v, begins, n, l2, a, c, wave, col, quad, [&] {
+                    if (!kAhead) return;
+                    if constexpr (READS) qr.arrive();
+                    kr.arrive(), vr.arrive();
+                    asm volatile("" : "+v"(flag));
+                });
             kept = begins || kept < 0.0f ? -1.0f : kept * __builtin_amdgcn_exp2f(l2 * (float)n);
         }
     }
@@ -705,9 +747,13 @@ struct Work {
     int64_t at, rh, r, env;        // at: with its segment; rh: row and head
     int     segment, h;
     template <typename Args>
-    __device__ __forceinline__ Work(const Args &a, int64_t id)
+    __device__ __forceinline__ Work(const Args &a, int64_t id) : Work(a, a.works <= gridDim.x ? neighbour(id, a.works) : id, 0)
     {
-        at = a.works <= gridDim.x ? neighbour(id, a.works) : id;
+    }
+    template <typename Args>
+    __device__ __forceinline__ Work(const Args &a, int64_t which, int)
+    {
+        at = which;
         // (a division's result is the same for all, but not known to be; rows x heads has 31 bits)
         rh = a.segments == 1 ? at : uniform(at / a.segments);
         segment = (int)(at - rh * a.segments);
@@ -720,7 +766,7 @@ struct Work {
 
 // Wavefronts of a SIMD, as many as the LDS of a workgroup lets the machine hold.
 constexpr int attention_wavefronts(int d, int type) { return d >= 96 ? type == TABX_F32 ? 2 : 4 : 3; }
-constexpr int attention_grad_wavefronts(int d, int type) { return d >= 96 ? 2 : type == TABX_F32 ? 2 : 3; }
+constexpr int attention_grad_wavefronts(int d, int type) { return d <= 64 ? 3 : type == TABX_F32 ? 2 : d == 128 && type == TABX_F16 ? 3 : 4; }
 
 // The launch arguments, fetched anew for what follows.  A wavefront has too few scalar registers for what all of a kernel
 // needs, and what is fetched once at the top is spilled to vector registers (a quarter of the gradients' instructions).
@@ -809,13 +855,9 @@ __global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tab
             const Args &a = again<Args>();
             const int64_t first = w.segment * a.segment, last = min(first + a.segment, a.ticks), size = a.keys * a.values;
             if (a.controlled && a.controlled[w.r] == 0) {
-                T *const gq = (T *)a.grad_q + w.of(a.gqs), *const gk = (T *)a.grad_k + w.of(a.gks), *const gv = (T *)a.grad_v + w.of(a.gvs);
-                for (int64_t t = first; t < last; ++t)
-                    for (int j = threadIdx.x; j < max(a.keys, a.values); j += A::THREADS) {
-                        if (a.grad_q && j < a.keys) gq[t * a.gqs.tick + j] = (T)0.0f;
-                        if (a.grad_k && j < a.keys) gk[t * a.gks.tick + j] = (T)0.0f;
-                        if (a.grad_v && j < a.values) gv[t * a.gvs.tick + j] = (T)0.0f;
-                    }
+                if (a.grad_q) A::clear_rows((T *)a.grad_q + w.of(a.gqs), a.gqs.tick, first, last, a.keys);
+                if (a.grad_k) A::clear_rows((T *)a.grad_k + w.of(a.gks), a.gks.tick, first, last, a.keys);
+                if (a.grad_v) A::clear_rows((T *)a.grad_v + w.of(a.gvs), a.gvs.tick, first, last, a.values);
                 if (a.grad_state_in && w.segment == 0)
                     for (int j = threadIdx.x; j < size; j += A::THREADS) a.grad_state_in[w.rh * size + j] = 0.0f;
                 continue;
@@ -887,34 +929,95 @@ __global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tab
             asm volatile("" : "+v"(l2), "+v"(col), "+v"(quad));
             turn ^= 1;
             if (threadIdx.x == 0) wild[turn] = 0;
-            __syncthreads();
+            lds_meet();
             A::store(k, kr);
             A::store(v, vr);
             const uint32_t odd = A::store(q, qr) | A::store(g, gr);
             if (__ballot(odd != 0) && lane == 0) wild[turn] = 1;
             const uint64_t begins = __ballot(flag != 0);
             if (kAhead && begin + C < last) fetch(begin + C);
-            __syncthreads();
+            lds_meet();
             const bool odd_one = wild[turn] != 0;
             if (again<Args>().grad_k) {
                 A::compare(within, v, g, begins, l2, again<Args>().scale, wave, col, quad);
-                __syncthreads();
+                lds_meet();
                 const Part a = to_k();
                 const Course c = course(begin, 1);
                 if (__builtin_expect(odd_one, 0)) A::template advance_slowly<true>(turned, begins, n, l2, a, c, wave, col, quad);
-                else A::template advance<true>(turned, within, v, g, q, begins, n, l2, a, c, wave, col, quad);
-                __syncthreads();
+                else A::template advance<true>(turned, within, v, g, q, begins, n, l2, a, c, wave, col, quad, [] {});
+                lds_meet();
             }
             A::compare(within, k, q, begins, l2, again<Args>().scale, wave, col, quad);
-            __syncthreads();
+            lds_meet();
             const Part a = to_v();
             const Course c = course(begin, 1);
             if (__builtin_expect(odd_one, 0)) A::template advance_slowly<true>(state, begins, n, l2, a, c, wave, col, quad);
-            else A::template advance<true>(state, within, k, q, g, begins, n, l2, a, c, wave, col, quad);
+            else A::template advance<true>(state, within, k, q, g, begins, n, l2, a, c, wave, col, quad, [] {});
         }
         // what is left for the state before the first tick, if that belongs to its episode
         const Args &a = again<Args>();
         if (a.grad_state_in && w.segment == 0)
+            A::store_state(state, a.grad_state_in + w.rh * (a.keys * a.values), a.keys, a.values, a.values, 1, a.fresh && a.ticks > 0 && a.fresh[w.env] != 0);
+    }
+}
+
+// The gradients, each by a workgroup of its own: neighbours, which share what they read.
+template <int D, int TYPE>
+__global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tabx_attention_grad_apart_kernel(const AttentionGradArgs)
+{
+    typedef Attention<D, TYPE> A;
+    typedef AttentionGradArgs Args;
+    typedef typename A::T T;
+    constexpr int bytes = sizeof(T);
+    __shared__ typename A::In q, k, v;
+    __shared__ typename A::Within within;
+    __shared__ int wild[2];
+    int turn = 0;
+    for (int64_t id = blockIdx.x; id < 3 * again<Args>().works; id += gridDim.x) {
+        const int64_t at = 3 * again<Args>().works <= gridDim.x ? neighbour(id, 3 * again<Args>().works) : id;
+        const int64_t which = uniform(at / 3);
+        const int role = (int)(at - 3 * which);
+        const Work w(again<Args>(), which, 0);
+        // grad_q: queries grad_out, keys v, values k; grad_k: queries v, keys grad_out, values q; grad_v: queries k, keys q,
+        // values grad_out
+        const auto part = [&] {
+            const Args &a = again<Args>();
+            const void *const xq = moved_on(a.q, w.of(a.qs), bytes), *const xk = moved_on(a.k, w.of(a.ks), bytes),
+                              *const xv = moved_on(a.v, w.of(a.vs), bytes), *const xg = moved_on(a.grad_out, w.of(a.os), bytes);
+            if (role == 0) return Part{xg, xv, xk, moved_on(a.grad_q, w.of(a.gqs), bytes), a.os.tick, a.vs.tick, a.ks.tick, a.gqs.tick, a.values, a.keys, 0, a.scale, 1.0f};
+            if (role == 1) return Part{xv, xg, xq, moved_on(a.grad_k, w.of(a.gks), bytes), a.vs.tick, a.os.tick, a.qs.tick, a.gks.tick, a.values, a.keys, 1, 1.0f, a.scale};
+            return Part{xk, xq, xg, a.grad_v ? moved_on(a.grad_v, w.of(a.gvs), bytes) : nullptr, a.ks.tick, a.qs.tick, a.os.tick, a.gvs.tick, a.keys, a.values, 1, 1.0f, a.scale};
+        };
+        const auto course = [&](int64_t begin) {
+            const Args &a = again<Args>();
+            return Course{a.fresh ? a.fresh + w.env : nullptr, a.envs, a.ticks, begin, role != 0};
+        };
+        typename A::State state;
+        float kept = 1.0f, decay;
+        int64_t first, last;
+        {
+            const Args &a = again<Args>();
+            if (role == 0 ? !a.grad_q : role == 1 ? !a.grad_k : !a.grad_v && !a.grad_state_in) continue;
+            const int64_t size = a.keys * a.values;
+            first = w.segment * a.segment, last = min(first + a.segment, a.ticks);
+            if (a.controlled && a.controlled[w.r] == 0) {
+                const Part p = part();
+                if (p.out) A::clear_rows(p.out, p.out_tick, first, last, p.values);
+                if (role == 2 && a.grad_state_in && w.segment == 0)
+                    for (int j = threadIdx.x; j < size; j += A::THREADS) a.grad_state_in[w.rh * size + j] = 0.0f;
+                continue;
+            }
+            decay = fmaxf(log2_decay(a.log_decay, w.h), -1e9f);
+            const float *const before = role == 0 ? a.states : a.grad_states, *const given = role == 0 ? a.state_in : a.grad_state_out;
+            const float *const from = before ? before + w.at * size : given ? given + w.rh * size : nullptr;
+            if (!from) A::clear(state);
+            else if (role == 2) A::load_state(state, from, a.keys, a.values, a.values, 1);
+            else A::load_state(state, from, a.values, a.keys, 1, a.values);
+        }
+        A::template go_through<true>(state, kept, q, k, v, within, wild, turn, part, course, first, last, decay);
+        // what is left for the state before the first tick, if that belongs to its episode
+        const Args &a = again<Args>();
+        if (role == 2 && a.grad_state_in && w.segment == a.segments - 1)
             A::store_state(state, a.grad_state_in + w.rh * (a.keys * a.values), a.keys, a.values, a.values, 1, a.fresh && a.ticks > 0 && a.fresh[w.env] != 0);
     }
 }

@@ -271,13 +271,18 @@ static int carry(AttentionArgs &a, int type, void *workspace, void *stream)
     return launch(tabx_attention_join_kernel, least(quotient_up(states, 256), kMostGroups), 256, a, stream);
 }
 
-template <int D>
-static int launch_attention_grad(const AttentionGradArgs &a, int type, void *stream)
+template <int D, int TYPE>
+static int launch_attention_grad(const AttentionGradArgs &a, void *stream)
 {
-    return launch(type == TABX_F32    ? tabx_attention_grad_kernel<D, TABX_F32>
-                  : type == TABX_BF16 ? tabx_attention_grad_kernel<D, TABX_BF16>
-                                      : tabx_attention_grad_kernel<D, TABX_F16>,
-                  least(a.works, kMostGroups), 4 * D, a, stream);
+    if constexpr (D <= 64 && TYPE != TABX_F32) return launch(tabx_attention_grad_kernel<D, TYPE>, least(a.works, kMostGroups), 4 * D, a, stream);
+    else return launch(tabx_attention_grad_apart_kernel<D, TYPE>, least(3 * a.works, kMostGroups), 4 * D, a, stream);
+}
+
+template <int D>
+static int attention_grad_of_type(const AttentionGradArgs &a, int type, void *stream)
+{
+    return type == TABX_F32 ? launch_attention_grad<D, TABX_F32>(a, stream) : type == TABX_BF16 ? launch_attention_grad<D, TABX_BF16>(a, stream)
+                                                                                                : launch_attention_grad<D, TABX_F16>(a, stream);
 }
 
 template <int TYPE, int VALUES, int LANES>
@@ -535,10 +540,10 @@ int tabx_linear_attention_backward(int64_t ticks, int64_t rows, int32_t heads, i
         }
     }
     const int width = form_width(key_width, value_width);
-    if (width == 32) return launch_attention_grad<32>(a, type, stream);
-    if (width == 64) return launch_attention_grad<64>(a, type, stream);
-    if (width == 96) return launch_attention_grad<96>(a, type, stream);
-    return launch_attention_grad<128>(a, type, stream);
+    if (width == 32) return attention_grad_of_type<32>(a, type, stream);
+    if (width == 64) return attention_grad_of_type<64>(a, type, stream);
+    if (width == 96) return attention_grad_of_type<96>(a, type, stream);
+    return attention_grad_of_type<128>(a, type, stream);
 }
 
 } // extern "C"
