@@ -573,28 +573,36 @@ def _heads(what, t, name, device, ticks=None):
     if code is None:
         _refuse(what, f"{name} is {t.dtype}, not one of float32, bfloat16, float16")
     shape, stride = t.shape, t.stride()
-    first, n = 0 if ticks is None else 1, len(shape)
+    n = len(shape)
+    first = 0 if ticks is None else 1
     if n < first + 2:
         _refuse(what, f"{name} has {n} dimensions")
-    if first and shape[0] != ticks:
-        _refuse(what, f"{name} has {shape[0]} ticks, not {ticks}")
-    if shape[-1] > _MOST or shape[-2] > _MOST:
-        _refuse(what, f"{name} has {shape[-2]} heads of {shape[-1]} elements")
+    heads, wide = shape[-2:]
+    if heads > _MOST or wide > _MOST:
+        _refuse(what, f"{name} has {heads} heads of {wide} elements")
     if t.get_device() != device:
         _elsewhere(what, t, name, device)
-    if shape[-1] > 1 and stride[-1] != 1:
+    if wide > 1 and stride[-1] != 1:
         _refuse(what, f"the elements of a head of {name} are not next to each other")
-    count, apart = 1, 0
-    for d in range(n - 3, first - 1, -1):
-        if shape[d] == 1:
-            continue
-        if count == 1:
-            apart = stride[d]
-        elif stride[d] != apart * count:
-            _refuse(what, f"the rows of {name} do not lie at equal distances")
-        count *= shape[d]
-    return (TabxHeads(t.data_ptr(), stride[0] if first and shape[0] > 1 else 0, apart,
-                      stride[-2] if shape[-2] > 1 else 0, code), count, shape[-2], shape[-1])
+    along = 0
+    if first:
+        if shape[0] != ticks:
+            _refuse(what, f"{name} has {shape[0]} ticks, not {ticks}")
+        if ticks > 1:
+            along = stride[0]
+    if n == first + 3:                         # (most are so)
+        count, apart = shape[first], stride[first]
+    else:
+        count, apart = 1, 0
+        for d in range(n - 3, first - 1, -1):
+            if shape[d] == 1:
+                continue
+            if count == 1:
+                apart = stride[d]
+            elif stride[d] != apart * count:
+                _refuse(what, f"the rows of {name} do not lie at equal distances")
+            count *= shape[d]
+    return TabxHeads(t.data_ptr(), along, apart, stride[-2], code), count, heads, wide
 
 
 def _same_heads(what, t, name, device, rows, heads, width, ticks=None):

@@ -88,7 +88,7 @@ struct StepArgs {
 
 // A state is a run of keys x values floats.  LANES lanes have a row's head (64: a whole wavefront); lane l has four
 // consecutive values of every (4 LANES / VALUES)-th line of the state, so that the lanes read and write 16 bytes each of
-// one run.  VALUES: the values rounded up to a power of two; lanes beyond the last value idle.
+// one run.  VALUES: the values, a multiple of four, rounded up to a power of two; lanes beyond the last value idle.
 template <int TYPE, int VALUES, int LANES>
 __global__ __launch_bounds__(256) void tabx_attention_step_kernel(const StepArgs a)
 {
@@ -107,39 +107,23 @@ __global__ __launch_bounds__(256) void tabx_attention_step_kernel(const StepArgs
                 *const v = (const T *)a.v + r * a.vs.row + h * a.vs.head + d;
         float *const state = a.state + w * a.keys * a.values + d;
         f32x4 value = {0.0f, 0.0f, 0.0f, 0.0f}, sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (count > 0) value = load_four<TYPE>(v);
+        for (int i = line; i < a.keys; i += LINES * AT_ONCE) {
+            f32x4 s[AT_ONCE];
+            float x[AT_ONCE], y[AT_ONCE];
 #pragma unroll
-        for (int n = 0; n < 4; ++n)
-            if (n < count) value[n] = (float)v[n];
-        if (a.values % 4 == 0) {
-            for (int i = line; i < a.keys; i += LINES * AT_ONCE) {
-                f32x4 s[AT_ONCE];
-                float x[AT_ONCE], y[AT_ONCE];
-#pragma unroll
-                for (int n = 0; n < AT_ONCE; ++n) {
-                    const int key = min(i + n * LINES, a.keys - 1);
-                    if (count > 0) s[n] = *(const Anywhere *)(state + key * a.values);
-                    x[n] = (float)k[key], y[n] = (float)q[key];
-                }
-#pragma unroll
-                for (int n = 0; n < AT_ONCE; ++n) {
-                    if (i + n * LINES >= a.keys || count <= 0) continue;
-                    const f32x4 old = forget ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : s[n] * e;
-                    const f32x4 now = {fmaf(x[n], value.x, old.x), fmaf(x[n], value.y, old.y), fmaf(x[n], value.z, old.z), fmaf(x[n], value.w, old.w)};
-                    *(Anywhere *)(state + (i + n * LINES) * a.values) = now;
-                    sum = f32x4{fmaf(y[n], now.x, sum.x), fmaf(y[n], now.y, sum.y), fmaf(y[n], now.z, sum.z), fmaf(y[n], now.w, sum.w)};
-                }
+            for (int n = 0; n < AT_ONCE; ++n) {
+                const int key = min(i + n * LINES, a.keys - 1);
+                if (count > 0) s[n] = *(const Anywhere *)(state + key * a.values);
+                x[n] = (float)k[key], y[n] = (float)q[key];
             }
-        } else {
-            for (int i = line; i < a.keys; i += LINES) {
-                const float x = (float)k[i], y = (float)q[i];
 #pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    if (n >= count) continue;
-                    float s = state[i * a.values + n];
-                    s = fmaf(x, value[n], forget ? 0.0f : e * s);
-                    state[i * a.values + n] = s;
-                    sum[n] = fmaf(y, s, sum[n]);
-                }
+            for (int n = 0; n < AT_ONCE; ++n) {
+                if (i + n * LINES >= a.keys || count <= 0) continue;
+                const f32x4 old = forget ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : s[n] * e;
+                const f32x4 now = {fmaf(x[n], value.x, old.x), fmaf(x[n], value.y, old.y), fmaf(x[n], value.z, old.z), fmaf(x[n], value.w, old.w)};
+                *(Anywhere *)(state + (i + n * LINES) * a.values) = now;
+                sum = f32x4{fmaf(y[n], now.x, sum.x), fmaf(y[n], now.y, sum.y), fmaf(y[n], now.z, sum.z), fmaf(y[n], now.w, sum.w)};
             }
         }
 #pragma unroll
@@ -149,13 +133,49 @@ __global__ __launch_bounds__(256) void tabx_attention_step_kernel(const StepArgs
         if (line == 0 && count > 0) {
             T *const out = (T *)a.out + r * a.os.row + h * a.os.head + d;
             sum *= a.scale;
-            if (count >= 4) {
-                store_four<TYPE>(out, sum);
-            } else {
+            store_four<TYPE>(out, sum);
+        }
+    }
+}
+
+// The same for values that are no multiple of four: a wavefront has a row's head, a lane one value (or two) of every
+// (64 / ACROSS)-th line.
+template <int TYPE, int ACROSS>
+__global__ __launch_bounds__(256) void tabx_attention_step_odd_kernel(const StepArgs a)
+{
+    typedef typename Element<TYPE>::one T;
+    constexpr int LINES = 64 / ACROSS, AT_ONCE = 8;
+    const int lane = (int)threadIdx.x & 63, line = lane / ACROSS;
+    for (int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); w < a.works; w += (int64_t)gridDim.x * 4) {
+        const int64_t r = (uint32_t)w / (uint32_t)a.heads;
+        const int h = (int)((uint32_t)w % (uint32_t)a.heads);
+        if (a.controlled && a.controlled[r] == 0) continue;
+        const bool forget = a.fresh && a.fresh[(uint32_t)r / (uint32_t)a.units] != 0;
+        const float e = decayed(log2_decay(a.log_decay, h), 1);
+        const T *const q = (const T *)a.q + r * a.qs.row + h * a.qs.head, *const k = (const T *)a.k + r * a.ks.row + h * a.ks.head,
+                *const v = (const T *)a.v + r * a.vs.row + h * a.vs.head;
+        for (int d = lane % ACROSS; d < a.values; d += ACROSS) {
+            float *const state = a.state + w * a.keys * a.values + d;
+            const float value = (float)v[d];
+            float sum = 0.0f;
+            for (int i = line; i < a.keys; i += LINES * AT_ONCE) {
+                float s[AT_ONCE], x[AT_ONCE], y[AT_ONCE];
 #pragma unroll
-                for (int n = 0; n < 3; ++n)
-                    if (n < count) out[n] = (T)sum[n];
+                for (int n = 0; n < AT_ONCE; ++n) {
+                    const int key = min(i + n * LINES, a.keys - 1);
+                    s[n] = state[key * a.values], x[n] = (float)k[key], y[n] = (float)q[key];
+                }
+#pragma unroll
+                for (int n = 0; n < AT_ONCE; ++n) {
+                    if (i + n * LINES >= a.keys) continue;
+                    const float now = fmaf(x[n], value, forget ? 0.0f : e * s[n]);
+                    state[(i + n * LINES) * a.values] = now;
+                    sum = fmaf(y[n], now, sum);
+                }
             }
+#pragma unroll
+            for (int n = ACROSS; n < 64; n *= 2) sum += __shfl_xor(sum, n);
+            if (line == 0) ((T *)a.out)[r * a.os.row + h * a.os.head + d] = (T)(sum * a.scale);
         }
     }
 }
@@ -1025,7 +1045,7 @@ __global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tab
 // The states that the segments leave become those before them, one behind the other: a thread per element.
 static __global__ __launch_bounds__(256) void tabx_attention_join_kernel(const AttentionArgs a)
 {
-    constexpr int AHEAD = 16;
+    constexpr int AHEAD = 32;
     const int64_t size = (int64_t)a.keys * a.values, all = a.rows * a.heads * size;
     for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < all; at += (int64_t)gridDim.x * 256) {
         const int64_t rh = at / size, d = at % size;

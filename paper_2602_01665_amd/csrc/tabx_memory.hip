@@ -174,6 +174,9 @@ static int rotary_in_runs(RotaryArgs a, bool interleaved, bool copies, void *str
     const int64_t runs = quotient_up(a.pairs, PAIRS), slots = runs + (copies ? quotient_up(a.width - 2 * a.pairs, PAIRS) : 0);
     if (a.heads > INT32_MAX / (2 * slots)) return TABX_ERR_SHAPE;
     a.row_angles = (int32_t)(runs * PAIRS);
+    const int behind = a.width - 2 * a.pairs;
+    a.last_run = copies && a.pairs >= PAIRS ? a.pairs - PAIRS : INT32_MAX;
+    a.last_plain = behind >= PAIRS ? behind - PAIRS : INT32_MAX;
     a.head_slots = (int32_t)slots, a.row_slots = (int32_t)(slots * a.heads);
     int64_t rows = 1024 / a.row_slots;             // four runs to a lane
     rows = least(rows < 1 ? 1 : rows, kRotaryAngles / a.row_angles);
@@ -285,6 +288,13 @@ static int attention_grad_of_type(const AttentionGradArgs &a, int type, void *st
                                                                                                 : launch_attention_grad<D, TABX_F16>(a, stream);
 }
 
+// Values that are no multiple of four: a lane has one of them.
+template <int TYPE, int ACROSS>
+static int launch_step_odd(const StepArgs &a, void *stream)
+{
+    return launch(tabx_attention_step_odd_kernel<TYPE, ACROSS>, least(quotient_up(a.works, 4), kMostGroups), 256, a, stream);
+}
+
 template <int TYPE, int VALUES, int LANES>
 static int launch_step(const StepArgs &a, void *stream)
 {
@@ -295,6 +305,11 @@ static int launch_step(const StepArgs &a, void *stream)
 template <int TYPE>
 static int attention_step(const StepArgs &a, void *stream)
 {
+    if (a.values % 4 != 0) {
+        if (a.values <= 8) return launch_step_odd<TYPE, 8>(a, stream);
+        if (a.values <= 16) return launch_step_odd<TYPE, 16>(a, stream);
+        return a.values <= 32 ? launch_step_odd<TYPE, 32>(a, stream) : launch_step_odd<TYPE, 64>(a, stream);
+    }
     if (a.values <= 4) return a.keys <= 16 ? launch_step<TYPE, 4, 8>(a, stream) : launch_step<TYPE, 4, 64>(a, stream);
     if (a.values <= 8) return a.keys <= 16 ? launch_step<TYPE, 8, 16>(a, stream) : launch_step<TYPE, 8, 64>(a, stream);
     if (a.values <= 16) return a.keys <= 32 ? launch_step<TYPE, 16, 16>(a, stream) : launch_step<TYPE, 16, 64>(a, stream);

@@ -19,6 +19,7 @@ struct RotaryArgs {
     int32_t     num_axes, heads, width, pairs;
     int32_t     group_rows, row_angles;               // rows of a workgroup; angles of a row in LDS, whole runs
     int32_t     row_slots, head_slots;                // runs of pairs or copied elements of a row, of a head
+    int32_t     last_run, last_plain;                 // where the last runs of a head start at the latest
     uint32_t    row_magic, head_magic, angle_magic;   // 2^32 / row_slots, head_slots, angles of a row, rounded up; 0: divide
     double      sign;              // of the angles, times the quarter turns of a radian
 };
@@ -98,12 +99,15 @@ __global__ __launch_bounds__(256) void tabx_rotary_kernel(const RotaryArgs a)
             const int slot = rest - head * a.head_slots;
             if (a.row_mask && a.row_mask[base + row] == 0) return;
             const bool turns = slot < turned;
-            const int first = turns ? (INTERLEAVED ? 2 : 1) * PAIRS * slot : 2 * a.pairs + PAIRS * (slot - turned);
+            // what is left of a head beyond whole runs is taken with what lies before it once more, where that is not
+            // overwritten meanwhile
+            const int pair = min(PAIRS * slot, a.last_run), plain = min(PAIRS * (slot - turned), a.last_plain);
+            const int first = turns ? (INTERLEAVED ? 2 : 1) * pair : 2 * a.pairs + plain;
             const T *const from = x + ((Offset)row * (Offset)a.x_row + (Offset)head * (Offset)a.x_head + first);
             n.to = (Offset)row * (Offset)a.y_row + (Offset)head * (Offset)a.y_head + first;
-            n.angle = row * a.row_angles + PAIRS * slot;
+            n.angle = row * a.row_angles + pair;
             if (turns) {
-                n.count = min(PAIRS, a.pairs - PAIRS * slot);
+                n.count = min(PAIRS, a.pairs - pair);
                 if (n.count == PAIRS) {            // (interleaved: the pairs' first half and second half)
                     n.u.load(from);
                     n.v.load(from + (INTERLEAVED ? PAIRS : a.pairs));
@@ -112,7 +116,7 @@ __global__ __launch_bounds__(256) void tabx_rotary_kernel(const RotaryArgs a)
                     n.v.load_some(from + (INTERLEAVED ? 1 : a.pairs), INTERLEAVED ? 2 : 1, n.count);
                 }
             } else {
-                const int some = min(PAIRS, behind - PAIRS * (slot - turned));
+                const int some = min(PAIRS, behind - plain);
                 n.count = -some;
                 if (some == PAIRS) n.u.load(from);
                 else n.u.load_some(from, 1, some);
