@@ -196,7 +196,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int chunk_of(int d, int type) { return type == TABX_BF16 && d > 32 ? 64 : 32; }
+// Ticks of a chunk.  Long ones spare steps, short ones room: 64 only where it pays and there are as many.
+constexpr int long_chunk(int d, int type) { return type == TABX_BF16 && d > 32 ? 64 : 32; }
 
 template <int N>
 __device__ __forceinline__ void split(bf16x4 (&part)[N], f32x4 v)
@@ -366,9 +367,9 @@ __device__ __forceinline__ T *moved_on(T *data, int64_t elements, int bytes)
     return (T *)((Byte *)data + elements * bytes);
 }
 
-template <int D, int TYPE>
+template <int D, int TYPE, int C>
 struct Attention {
-    static constexpr int C = chunk_of(D, TYPE), IN = Parts<TYPE>::in, MID = Parts<TYPE>::mid;
+    static constexpr int IN = Parts<TYPE>::in, MID = Parts<TYPE>::mid;
     static constexpr bool kAhead = D < 96 || TYPE == TABX_F32;
     static constexpr int WAVES = D / 16, THREADS = 64 * WAVES, PASSES = C * D / 8 / THREADS, TILES = D / 16;
     typedef typename Element<TYPE>::one T;
@@ -801,10 +802,10 @@ __device__ __forceinline__ const Args &again()
 
 // A workgroup goes through its ticks with the state in registers.  CARRY: nothing is read, the states that the segments
 // would leave of nothing are.
-template <int D, int TYPE, bool CARRY>
+template <int D, int TYPE, int C, bool CARRY>
 __global__ __launch_bounds__(4 * D, attention_wavefronts(D, TYPE)) void tabx_attention_kernel(const AttentionArgs)
 {
-    typedef Attention<D, TYPE> A;
+    typedef Attention<D, TYPE, C> A;
     typedef AttentionArgs Args;
     __shared__ typename A::In q, k, v;
     __shared__ typename A::Within within;
@@ -851,13 +852,13 @@ __global__ __launch_bounds__(4 * D, attention_wavefronts(D, TYPE)) void tabx_att
 
 // The gradients: forwards through the ticks for grad_q, then backwards for grad_k and grad_v, which read the same rows,
 // and the state's; the last chunk forwards is the first one backwards, and what was read is still in the caches.
-template <int D, int TYPE>
+template <int D, int TYPE, int C>
 __global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tabx_attention_grad_kernel(const AttentionGradArgs)
 {
-    typedef Attention<D, TYPE> A;
+    typedef Attention<D, TYPE, C> A;
     typedef AttentionGradArgs Args;
     typedef typename A::T T;
-    constexpr int C = A::C, bytes = sizeof(T);
+    constexpr int bytes = sizeof(T);
     constexpr bool kAhead = false;
     __shared__ typename A::In q, k, v, g;
     __shared__ typename A::Within within;
@@ -982,10 +983,10 @@ __global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tab
 }
 
 // The gradients, each by a workgroup of its own: neighbours, which share what they read.
-template <int D, int TYPE>
+template <int D, int TYPE, int C>
 __global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tabx_attention_grad_apart_kernel(const AttentionGradArgs)
 {
-    typedef Attention<D, TYPE> A;
+    typedef Attention<D, TYPE, C> A;
     typedef AttentionGradArgs Args;
     typedef typename A::T T;
     constexpr int bytes = sizeof(T);

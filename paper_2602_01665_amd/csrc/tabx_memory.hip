@@ -244,13 +244,21 @@ static int64_t attention_workspace(int64_t ticks, int64_t rows, int32_t heads, i
     return 2 * carried_bytes(segments_of(ticks, rows, heads, keys, values), rows, heads, keys, values);
 }
 
+template <bool CARRY, int D, int TYPE>
+static int launch_attention_of(const AttentionArgs &a, void *stream)
+{
+    constexpr int chunk = long_chunk(D, TYPE);
+    const int64_t groups = least(a.works, kMostGroups);
+    if constexpr (chunk > 32 && !CARRY)
+        if (a.ticks <= 32) return launch(tabx_attention_kernel<D, TYPE, 32, CARRY>, groups, 4 * D, a, stream);
+    return launch(tabx_attention_kernel<D, TYPE, chunk, CARRY>, groups, 4 * D, a, stream);
+}
+
 template <bool CARRY, int D>
 static int launch_attention(const AttentionArgs &a, int type, void *stream)
 {
-    return launch(type == TABX_F32    ? tabx_attention_kernel<D, TABX_F32, CARRY>
-                  : type == TABX_BF16 ? tabx_attention_kernel<D, TABX_BF16, CARRY>
-                                      : tabx_attention_kernel<D, TABX_F16, CARRY>,
-                  least(a.works, kMostGroups), 4 * D, a, stream);
+    return type == TABX_F32 ? launch_attention_of<CARRY, D, TABX_F32>(a, stream) : type == TABX_BF16 ? launch_attention_of<CARRY, D, TABX_BF16>(a, stream)
+                                                                                                     : launch_attention_of<CARRY, D, TABX_F16>(a, stream);
 }
 
 template <bool CARRY>
@@ -274,11 +282,20 @@ static int carry(AttentionArgs &a, int type, void *workspace, void *stream)
     return launch(tabx_attention_join_kernel, least(quotient_up(states, 256), kMostGroups), 256, a, stream);
 }
 
+template <int D, int TYPE, int C>
+static int launch_attention_grad_of(const AttentionGradArgs &a, void *stream)
+{
+    if constexpr (D <= 64 && TYPE != TABX_F32) return launch(tabx_attention_grad_kernel<D, TYPE, C>, least(a.works, kMostGroups), 4 * D, a, stream);
+    else return launch(tabx_attention_grad_apart_kernel<D, TYPE, C>, least(3 * a.works, kMostGroups), 4 * D, a, stream);
+}
+
 template <int D, int TYPE>
 static int launch_attention_grad(const AttentionGradArgs &a, void *stream)
 {
-    if constexpr (D <= 64 && TYPE != TABX_F32) return launch(tabx_attention_grad_kernel<D, TYPE>, least(a.works, kMostGroups), 4 * D, a, stream);
-    else return launch(tabx_attention_grad_apart_kernel<D, TYPE>, least(3 * a.works, kMostGroups), 4 * D, a, stream);
+    constexpr int chunk = long_chunk(D, TYPE);
+    if constexpr (chunk > 32)
+        if (a.ticks <= 32) return launch_attention_grad_of<D, TYPE, 32>(a, stream);
+    return launch_attention_grad_of<D, TYPE, chunk>(a, stream);
 }
 
 template <int D>
