@@ -43,6 +43,11 @@ struct AttentionArgs {
     float       scale_read, scale_added;   // of what is read, of what is taken in
 };
 
+// What a launch works on: one attention, or two of the same sizes side by side (blockIdx.y).
+struct AttentionPair {
+    AttentionArgs of[2];
+};
+
 // The way back: all that the three attentions of the gradients need.
 struct AttentionGradArgs {
     const void *q, *k, *v, *grad_out;
@@ -803,32 +808,32 @@ __device__ __forceinline__ const Args &again()
 // A workgroup goes through its ticks with the state in registers.  CARRY: nothing is read, the states that the segments
 // would leave of nothing are.
 template <int D, int TYPE, int C, bool CARRY>
-__global__ __launch_bounds__(4 * D, attention_wavefronts(D, TYPE)) void tabx_attention_kernel(const AttentionArgs)
+__global__ __launch_bounds__(4 * D, attention_wavefronts(D, TYPE)) void tabx_attention_kernel(const AttentionPair)
 {
     typedef Attention<D, TYPE, C> A;
-    typedef AttentionArgs Args;
+    const auto mine = []() -> const AttentionArgs & { return again<AttentionPair>().of[blockIdx.y]; };
     __shared__ typename A::In q, k, v;
     __shared__ typename A::Within within;
     __shared__ int wild[2];
     int turn = 0;
-    for (int64_t id = blockIdx.x; id < again<Args>().works; id += gridDim.x) {
-        const Work w(again<Args>(), id);
+    for (int64_t id = blockIdx.x; id < mine().works; id += gridDim.x) {
+        const Work w(mine(), id);
         const auto part = [&] {
-            const Args &a = again<Args>();
+            const AttentionArgs &a = mine();
             constexpr int bytes = sizeof(typename A::T);
             return Part{moved_on(a.q, w.of(a.qs), bytes), moved_on(a.k, w.of(a.ks), bytes), moved_on(a.v, w.of(a.vs), bytes),
                         a.out ? moved_on(a.out, w.of(a.os), bytes) : nullptr, a.qs.tick, a.ks.tick, a.vs.tick, a.os.tick, a.keys, a.values,
                         a.backward, a.scale_read, a.scale_added};
         };
         const auto course = [&](int64_t begin) {
-            const Args &a = again<Args>();
+            const AttentionArgs &a = mine();
             return Course{a.fresh ? a.fresh + w.env : nullptr, a.envs, a.ticks, begin, a.backward};
         };
         typename A::State state;
         float kept = 1.0f, decay;
         int64_t first, last;
         {
-            const Args &a = again<Args>();
+            const AttentionArgs &a = mine();
             if (CARRY && w.segment == a.segments - 1) continue;        // (nothing comes behind it)
             if (a.controlled && a.controlled[w.r] == 0) continue;
             decay = fmaxf(log2_decay(a.log_decay, w.h), -1e9f);        // (all at once, and none of no ticks)
@@ -839,7 +844,7 @@ __global__ __launch_bounds__(4 * D, attention_wavefronts(D, TYPE)) void tabx_att
             first = w.segment * a.segment, last = min(first + a.segment, a.ticks);
         }
         A::template go_through<!CARRY>(state, kept, q, k, v, within, wild, turn, part, course, first, last, decay);
-        const Args &a = again<Args>();
+        const AttentionArgs &a = mine();
         const int64_t size = a.keys * a.values;
         if (CARRY) {
             A::store_state(state, a.carried + w.at * size, a.keys, a.values, a.values, 1, false);
@@ -1044,8 +1049,9 @@ __global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tab
 }
 
 // The states that the segments leave become those before them, one behind the other: a thread per element.
-static __global__ __launch_bounds__(256) void tabx_attention_join_kernel(const AttentionArgs a)
+static __global__ __launch_bounds__(256) void tabx_attention_join_kernel(const AttentionPair pair)
 {
+    const AttentionArgs &a = pair.of[blockIdx.y];
     constexpr int AHEAD = 32;
     const int64_t size = (int64_t)a.keys * a.values, all = a.rows * a.heads * size;
     for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < all; at += (int64_t)gridDim.x * 256) {
@@ -1054,15 +1060,18 @@ static __global__ __launch_bounds__(256) void tabx_attention_join_kernel(const A
         float s = a.state_in ? a.state_in[rh * size + d] : 0.0f;
         float *const of = a.carried + rh * a.segments * size + d;
         const float *const kept = a.kept + rh * a.segments;
-        for (int n = 0; n < a.segments; n += AHEAD) {          // (what the last one leaves is the attention's to work out)
-            float left[AHEAD];
+        for (int n = 0; n < a.segments; n += AHEAD) {          // (the last one's, which is not there, goes nowhere)
+            float left[AHEAD], part[AHEAD];        // all of them before the first store, behind which they would be loaded one by one
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i) left[i] = n + i < a.segments - 1 ? of[(n + i) * size] : 0.0f;
+            for (int i = 0; i < AHEAD; ++i) {
+                const int at = min(n + i, a.segments - 1);
+                left[i] = of[at * size], part[i] = kept[at];
+            }
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) {
                 if (n + i >= a.segments) break;
                 of[(n + i) * size] = s;
-                if (n + i < a.segments - 1) s = kept[n + i] < 0.0f ? left[i] : fmaf(kept[n + i], s, left[i]);
+                s = part[i] < 0.0f ? left[i] : fmaf(part[i], s, left[i]);
             }
         }
     }

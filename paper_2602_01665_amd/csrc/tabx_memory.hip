@@ -220,7 +220,7 @@ static int form_width(int32_t keys, int32_t values)
 struct Segments {
     int64_t count, ticks;
 };
-constexpr int64_t kSegmentTicks = 128;             // at least; a multiple of every chunk
+constexpr int64_t kSegmentTicks = 64;              // at least; a multiple of every chunk
 
 static Segments segments_of(int64_t ticks, int64_t rows, int32_t heads, int32_t keys, int32_t values)
 {
@@ -244,42 +244,52 @@ static int64_t attention_workspace(int64_t ticks, int64_t rows, int32_t heads, i
     return 2 * carried_bytes(segments_of(ticks, rows, heads, keys, values), rows, heads, keys, values);
 }
 
+// One or two attentions of the same sizes.
+static int launch_pair(void (*kernel)(AttentionPair), int64_t groups, int threads, const AttentionPair &pair, int count, void *stream)
+{
+    void *args[] = {(void *)&pair};
+    return launched(hipLaunchKernel((const void *)kernel, dim3((unsigned)groups, (unsigned)count), dim3((unsigned)threads), args, 0, (hipStream_t)stream));
+}
+
 template <bool CARRY, int D, int TYPE>
-static int launch_attention_of(const AttentionArgs &a, void *stream)
+static int launch_attention_of(const AttentionPair &pair, int count, void *stream)
 {
     constexpr int chunk = long_chunk(D, TYPE);
-    const int64_t groups = least(a.works, kMostGroups);
+    const int64_t groups = least(pair.of[0].works, kMostGroups);
     if constexpr (chunk > 32 && !CARRY)
-        if (a.ticks <= 32) return launch(tabx_attention_kernel<D, TYPE, 32, CARRY>, groups, 4 * D, a, stream);
-    return launch(tabx_attention_kernel<D, TYPE, chunk, CARRY>, groups, 4 * D, a, stream);
+        if (pair.of[0].ticks <= 32) return launch_pair(tabx_attention_kernel<D, TYPE, 32, CARRY>, groups, 4 * D, pair, count, stream);
+    return launch_pair(tabx_attention_kernel<D, TYPE, chunk, CARRY>, groups, 4 * D, pair, count, stream);
 }
 
 template <bool CARRY, int D>
-static int launch_attention(const AttentionArgs &a, int type, void *stream)
+static int launch_attention(const AttentionPair &pair, int count, int type, void *stream)
 {
-    return type == TABX_F32 ? launch_attention_of<CARRY, D, TABX_F32>(a, stream) : type == TABX_BF16 ? launch_attention_of<CARRY, D, TABX_BF16>(a, stream)
-                                                                                                     : launch_attention_of<CARRY, D, TABX_F16>(a, stream);
+    if (type == TABX_F32) return launch_attention_of<CARRY, D, TABX_F32>(pair, count, stream);
+    return type == TABX_BF16 ? launch_attention_of<CARRY, D, TABX_BF16>(pair, count, stream) : launch_attention_of<CARRY, D, TABX_F16>(pair, count, stream);
 }
 
 template <bool CARRY>
-static int attention_of_width(const AttentionArgs &a, int type, void *stream)
+static int attention_of_width(const AttentionPair &pair, int count, int type, void *stream)
 {
-    const int width = form_width(a.keys, a.values);
-    if (width == 32) return launch_attention<CARRY, 32>(a, type, stream);
-    if (width == 64) return launch_attention<CARRY, 64>(a, type, stream);
-    if (width == 96) return launch_attention<CARRY, 96>(a, type, stream);
-    return launch_attention<CARRY, 128>(a, type, stream);
+    const int width = form_width(pair.of[0].keys, pair.of[0].values);
+    if (width == 32) return launch_attention<CARRY, 32>(pair, count, type, stream);
+    if (width == 64) return launch_attention<CARRY, 64>(pair, count, type, stream);
+    if (width == 96) return launch_attention<CARRY, 96>(pair, count, type, stream);
+    return launch_attention<CARRY, 128>(pair, count, type, stream);
 }
 
-// The states before each segment, into the workspace.
-static int carry(AttentionArgs &a, int type, void *workspace, void *stream)
+// The states before each segment of one or two attentions, each into its part of the workspace.
+static int carry(AttentionPair &pair, int count, int type, void *workspace, int64_t bytes, void *stream)
 {
-    a.carried = (float *)workspace;
-    a.kept = a.carried + a.works * a.keys * a.values;
-    const int rc = attention_of_width<true>(a, type, stream);
+    for (int n = 0; n < count; ++n) {
+        AttentionArgs &a = pair.of[n];
+        a.carried = (float *)((char *)workspace + n * bytes);
+        a.kept = a.carried + a.works * a.keys * a.values;
+    }
+    const int rc = attention_of_width<true>(pair, count, type, stream);
     if (rc) return rc;
-    const int64_t states = a.rows * a.heads * a.keys * a.values;
-    return launch(tabx_attention_join_kernel, least(quotient_up(states, 256), kMostGroups), 256, a, stream);
+    const AttentionArgs &a = pair.of[0];
+    return launch_pair(tabx_attention_join_kernel, least(quotient_up(a.rows * a.heads * a.keys * a.values, 256), kMostGroups), 256, pair, count, stream);
 }
 
 template <int D, int TYPE, int C>
@@ -507,8 +517,9 @@ int tabx_linear_attention(int64_t ticks, int64_t rows, int32_t heads, int32_t ke
     a.ticks = ticks, a.rows = rows, a.envs = rows / units, a.works = rows * heads * s.count, a.segment = s.ticks;
     a.segments = (int32_t)s.count, a.heads = heads, a.units = units, a.keys = key_width, a.values = value_width;
     a.scale_read = scale, a.scale_added = 1.0f;
-    if (s.count > 1 && (rc = carry(a, type, workspace, stream))) return rc;
-    return attention_of_width<false>(a, type, stream);
+    AttentionPair pair = {{a}};
+    if (s.count > 1 && (rc = carry(pair, 1, type, workspace, 0, stream))) return rc;
+    return attention_of_width<false>(pair, 1, type, stream);
 }
 
 int tabx_linear_attention_backward(int64_t ticks, int64_t rows, int32_t heads, int32_t key_width, int32_t value_width,
@@ -558,18 +569,21 @@ int tabx_linear_attention_backward(int64_t ticks, int64_t rows, int32_t heads, i
         c.log_decay = log_decay, c.fresh = fresh, c.controlled = controlled;
         c.ticks = a.ticks, c.rows = a.rows, c.envs = a.envs, c.works = a.works, c.segment = a.segment;
         c.segments = a.segments, c.heads = heads, c.units = units, c.keys = key_width, c.values = value_width;
+        AttentionPair pair = {};
+        int count = 0;
         if (grad_q) {
             c.k = a.k, c.v = a.v, c.ks = a.ks, c.vs = a.vs;
             c.state_in = state_in, c.scale_added = 1.0f;
-            if ((rc = carry(c, type, workspace, stream))) return rc;
-            a.states = c.carried;
+            pair.of[count++] = c;
         }
         if (grad_k || grad_v || grad_state_in) {
             c.k = a.q, c.v = a.grad_out, c.ks = a.qs, c.vs = a.os;
             c.state_in = grad_state_out, c.scale_added = scale, c.backward = 1;
-            if ((rc = carry(c, type, (char *)workspace + carried_bytes(s, rows, heads, key_width, value_width), stream))) return rc;
-            a.grad_states = c.carried;
+            pair.of[count++] = c;
         }
+        if ((rc = carry(pair, count, type, workspace, carried_bytes(s, rows, heads, key_width, value_width), stream))) return rc;
+        if (grad_q) a.states = pair.of[0].carried;
+        a.grad_states = pair.of[count - 1].carried;            // (not looked at where only grad_q is wanted)
     }
     const int width = form_width(key_width, value_width);
     if (width == 32) return attention_grad_of_type<32>(a, type, stream);
