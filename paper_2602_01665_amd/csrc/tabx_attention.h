@@ -188,10 +188,11 @@ __global__ __launch_bounds__(256) void tabx_attention_step_odd_kernel(const Step
 // --- many ticks ---------------------------------------------------------------------------------
 
 // The products run in the matrix cores in bf16 with sums in 32 bits, where every 32-bit operand stands as the sum of parts
-// of 8 bits each: bf16 inputs are one part, f16 ones two (both exact), f32 ones three; what lies between (the products of
-// queries and keys, the state, the faded values) is cut into two parts, three for f32.  Of the parts' products those are taken
-// that are above the last part's own rounding, so that 2^-16 of a term is lost, 2^-23 for f32 (a term's rounding to the
-// output is 2^-8, 2^-11, 2^-24), and nothing can leave the range of 32 bits that 32 bits would hold.
+// of 8 bits each: bf16 inputs are one part, f16 ones two (both exact), f32 ones three; what lies between on the way to an
+// output (the products of queries and keys, the state) is cut into two parts, three for f32, so that 2^-16 of a term is lost,
+// 2^-23 for f32, where the output's own rounding is 2^-8, 2^-11, 2^-24; what goes into the state, which is kept in 32 bits,
+// always into three.  Of the parts' products those are taken that are above the last part's rounding.  Nothing leaves the
+// range of 32 bits that 32 bits would hold.
 template <int TYPE> struct Parts {
     static constexpr int in = TYPE == TABX_BF16 ? 1 : TYPE == TABX_F16 ? 2 : 3;
     static constexpr int mid = TYPE == TABX_F32 ? 3 : 2;
@@ -541,14 +542,20 @@ struct Attention {
             }
         }
         __builtin_amdgcn_sched_barrier(0);
-        // the values faded by the ticks behind theirs; those of episodes that have ended count no more
+        // the values faded by the ticks behind theirs, in as many parts as the state has digits; those of episodes that have
+        // ended count no more
         const int newest = begins ? 63 - __builtin_clzll(begins) : 0;
         const float left = __builtin_amdgcn_exp2f(l2 * (float)n);
         const Powers power(l2);
-        bf16x8 faded[C / 32][MID];
+#pragma unroll
+        for (int s = 0; s < TILES; ++s) {
+            if (begins) state[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            else state[s] *= left;
+        }
 #pragma unroll
         for (int b = 0; b < C / 32; ++b) {
-            bf16x4 part[2][MID];
+            if (32 * b >= n) continue;
+            bf16x4 part[2][3];
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 f32x4 x;
@@ -574,21 +581,15 @@ struct Attention {
                 }
                 split(part[half], x);
             }
+            bf16x8 faded[3];
 #pragma unroll
-            for (int m = 0; m < MID; ++m) faded[b][m] = join(part[0][m], part[1][m]);
-        }
+            for (int m = 0; m < 3; ++m) faded[m] = join(part[0][m], part[1][m]);
 #pragma unroll
-        for (int s = 0; s < TILES; ++s) {
-            f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (!begins) x = state[s] * left;
-#pragma unroll
-            for (int b = 0; b < C / 32; ++b) {
-                if (32 * b >= n) continue;
+            for (int s = 0; s < TILES; ++s) {
                 bf16x8 y[IN];
                 k.across(y, 32 * b, 16 * s, col, quad);
-                x = multiply(y, faded[b], x);
+                state[s] = multiply(y, faded, state[s]);
             }
-            state[s] = x;
         }
     }
 

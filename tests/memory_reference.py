@@ -175,8 +175,9 @@ def attention(q, k, v, log_decay, scale, fresh, state):
             mag[t] = abs(scale) * (x[t].abs()[..., :, None] * S).sum(-2)
     loose = _loose(T, K, log_decay, q.dtype)
     tiny = 2.0 ** -120
+    exact = _loose(T, K, log_decay, torch.float32)             # the state is kept in 32 bits, whatever goes in
     return {"out": (out, rounded(loose * mag + tiny, out, q.dtype)),
-            "state_out": (final, loose[..., None] * S + tiny)}
+            "state_out": (final, exact[..., None] * S + tiny)}
 
 
 def attention_grad(q, k, v, log_decay, scale, fresh, state, grad_out, grad_state):
@@ -203,7 +204,8 @@ def attention_grad(q, k, v, log_decay, scale, fresh, state, grad_out, grad_state
 
     value, mag = run(_same), run(torch.abs)
     out = {n: (value[n], rounded(loose * mag[n] + tiny, value[n], q.dtype)) for n in ("grad_q", "grad_k", "grad_v")}
-    out["grad_state_in"] = (value["grad_state_in"], loose[..., None] * mag["grad_state_in"] + tiny)
+    exact = _loose(T, max(K, v.shape[-1]), log_decay, torch.float32)
+    out["grad_state_in"] = (value["grad_state_in"], exact[..., None] * mag["grad_state_in"] + tiny)
     return out
 
 
