@@ -112,17 +112,19 @@ __global__ __launch_bounds__(threads_of(LANES)) void tabx_rms_kernel(const RmsAr
 #pragma unroll
             for (int q = 0; q < PIECES; ++q) v[q] += r[q];
         }
-        if (a.sum) {
-            round_to(v, a.sum_type);
-            if (a.stream) store_row<true>(v, a.sum, a.sum_type, h.at * a.sum_stride, cut, a.width);
-            else store_row(v, a.sum, a.sum_type, h.at * a.sum_stride, cut, a.width);
-        }
+        if (a.sum) round_to(v, a.sum_type);
         const f32x4 last = cut.counted(v[PIECES - 1]);
         f32x4 squares = last * last;
 #pragma unroll
         for (int q = 0; q < PIECES - 1; ++q) squares = fma4(v[q], v[q], squares);
         const float rstd = rsqrtf(fmaf(row_sum<LANES>(sum_of(squares), slots[turn]), a.inv_width, a.eps));
         if (a.rstd && cut.lane == 0) a.rstd[h.at] = rstd;
+        // (the sum may lie where x or the residual does: not before all of the team has the row's last elements, which
+        // several lanes read)
+        if (a.sum) {
+            if (a.stream) store_row<true>(v, a.sum, a.sum_type, h.at * a.sum_stride, cut, a.width);
+            else store_row(v, a.sum, a.sum_type, h.at * a.sum_stride, cut, a.width);
+        }
         if (a.y_type == TABX_E4M3) {
             // y / scale is (s w) (448 / largest |s w|): rstd is in both and need not be rounded into either.  (Elements that
             // lie in two pieces are as large in both.)
