@@ -590,8 +590,8 @@ typedef struct TabxAxis {
  * Elements from 2 P on are copied.  The gradient of x is the same call with `inverse` on the gradient
  * of y.  frequency: device [P] f64, radians per unit of position.  row_mask: as in tabx_rms_norm.  A position
  * that is not finite gives NaN.  x and y have the same type (TABX_ERR_SHAPE); y may be x itself (same data and
- * strides).  1 <= num_axes <= TABX_ROTARY_MAX_AXES, heads >= 1, 2 <= width <= TABX_ROTARY_MAX_WIDTH,
- * 2 <= 2 P <= width (TABX_ERR_SHAPE).  tick_stride is not looked at. */
+ * strides, else TABX_ERR_SHAPE).  1 <= num_axes <= TABX_ROTARY_MAX_AXES, heads >= 1, 2 <= width <=
+ * TABX_ROTARY_MAX_WIDTH, heads * width <= 2^30, 2 <= 2 P <= width (TABX_ERR_SHAPE).  tick_stride is not looked at. */
 int tabx_rotary(int64_t rows, int32_t heads, int32_t width, const TabxHeads *x,
                 const uint8_t *row_mask, const TabxAxis *axes, int32_t num_axes,
                 const double *frequency, int32_t interleaved, int32_t inverse, const TabxHeads *y,

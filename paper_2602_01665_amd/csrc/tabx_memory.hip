@@ -172,7 +172,6 @@ template <int TYPE, int PAIRS>
 static int rotary_in_runs(RotaryArgs a, bool interleaved, bool copies, void *stream)
 {
     const int64_t runs = quotient_up(a.pairs, PAIRS), slots = runs + (copies ? quotient_up(a.width - 2 * a.pairs, PAIRS) : 0);
-    if (a.heads > INT32_MAX / (2 * slots)) return TABX_ERR_SHAPE;
     a.row_angles = (int32_t)(runs * PAIRS);
     const int behind = a.width - 2 * a.pairs;
     a.last_run = copies && a.pairs >= PAIRS ? a.pairs - PAIRS : INT32_MAX;
@@ -433,6 +432,7 @@ int tabx_rotary(int64_t rows, int32_t heads, int32_t width, const TabxHeads *x, 
 {
     using namespace tabx;
     if (rows < 0 || rows > (int64_t)1 << 40 || heads < 1 || width < 2 || width > TABX_ROTARY_MAX_WIDTH) return TABX_ERR_SHAPE;
+    if (heads > (1 << 30) / width) return TABX_ERR_SHAPE;
     if (num_axes < 1 || num_axes > TABX_ROTARY_MAX_AXES) return TABX_ERR_SHAPE;
     if (!axes) return TABX_ERR_NULL;
     RotaryArgs a = {};
@@ -453,6 +453,7 @@ int tabx_rotary(int64_t rows, int32_t heads, int32_t width, const TabxHeads *x, 
         if ((rc = check_floats(axes[n].position, false))) return rc;
     if ((rc = check_heads(x, 1, rows, heads, width, false)) || (rc = check_heads(y, 1, rows, heads, width, true))) return rc;
     if (x->type != y->type) return TABX_ERR_SHAPE;
+    if (x->data == y->data && (x->row_stride != y->row_stride || x->head_stride != y->head_stride)) return TABX_ERR_SHAPE;
     if (!frequency) return TABX_ERR_NULL;
     if (!on_boundary(frequency, 8)) return TABX_ERR_ALIGN;
     a.x = x->data, a.x_row = x->row_stride, a.x_head = x->head_stride;

@@ -79,7 +79,8 @@ def test_rotary(B):
                dict(a=axes((FAKE, 1, 1, 4))), dict(a=axes((FAKE, 4, 0, 4))), dict(a=axes((FAKE, 4, 4, 4))),
                dict(a=axes((FAKE, 4, 1, 2 ** 31 - 1), (FAKE, 4, 1, 2 ** 31 - 1))),
                dict(x=heads(B, 0, 64, 16, 3)), dict(x=heads(B, 0, 64, 16, 1)), dict(x=heads(B, 0, -64, 16)), dict(x=heads(B, 0, 1 << 60, 16)),
-               dict(y=heads(B, 0, 31, 16)), dict(y=heads(B, 0, 64, 15)), dict(y=heads(B, 0, 0, 16)), dict(y=heads(B, 0, 16, 16))):
+               dict(y=heads(B, 0, 31, 16)), dict(y=heads(B, 0, 64, 15)), dict(y=heads(B, 0, 0, 16)), dict(y=heads(B, 0, 16, 16)),
+               dict(h=1 << 27, width=16), dict(x=heads(B, 0, 96, 16)), dict(x=heads(B, 0, 64, 24))):
         assert call(**kw) == SHAPE, kw
     assert call(x=heads(B, 0, 64, 16, 0, None)) == NULL and call(freq=None) == NULL and call(a=axes((None, 4, 1, 4))) == NULL
     assert B._lib.tabx_rotary(6, 2, 16, None, None, axes((FAKE, 4, 1, 4)), 1, FAKE, 0, 0, heads(B, 0, 64, 16), None) == NULL
