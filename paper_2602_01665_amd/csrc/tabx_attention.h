@@ -261,12 +261,13 @@ struct Eight {
     }
 };
 
-// Not 0 in a bit of its own if one of them is not finite (an exponent of ones carries).
+// Not 0 in a bit of its own if one of them is not finite (an exponent of ones carries), or, of 32 bits, so large that its
+// first part would not be.
 template <int TYPE>
 __device__ __forceinline__ uint32_t not_finite(const Eight<TYPE> &e)
 {
     constexpr uint32_t exponent = TYPE == TABX_F32 ? 0x7f800000u : TYPE == TABX_BF16 ? 0x7f807f80u : 0x7c007c00u;
-    constexpr uint32_t one = TYPE == TABX_F32 ? 0x00800000u : TYPE == TABX_BF16 ? 0x00800080u : 0x04000400u;
+    constexpr uint32_t one = TYPE == TABX_F32 ? 0x01000000u : TYPE == TABX_BF16 ? 0x00800080u : 0x04000400u;
     uint32_t found = 0;
 #pragma unroll
     for (int n = 0; n < (TYPE == TABX_F32 ? 2 : 1); ++n)

@@ -303,6 +303,20 @@ def test_what_is_not_finite_stays_in_its_episode(B, dtype, what, T):
         M.near(after[0, 0], clean["state_out"][0][0, 0], clean["state_out"][1][0, 0], (name, t))
 
 
+def test_the_largest_values_stay_in_their_episode(B):
+    """Finite ones whose 16-bit part is not: what comes before them, and the next episode, is as it would be."""
+    T, R, H, K, V = 50, 1, 1, 16, 16
+    d = make(21, T, R, H, K, V, torch.float32, ends=0.0)
+    d["fresh"][30] = 1
+    clean = expected(d)
+    most = torch.finfo(torch.float32).max
+    d["v"][20, 0, 0, 5], d["k"][25, 0, 0, 2] = most, -most
+    out = M.f64(forward(B, on_gpu(d))["out"])
+    value, bound = clean["out"]
+    for t in (slice(0, 20), slice(30, T)):
+        M.near(out[t], value[t], bound[t], t)
+
+
 def test_gradients_against_differences(B):
     """The 64-bit gradients of the reference are the slopes of its sums, and the call's are those."""
     T, R, H, K, V = 9, 2, 2, 4, 3
