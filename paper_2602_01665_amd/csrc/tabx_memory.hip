@@ -294,8 +294,20 @@ static int carry(AttentionPair &pair, int count, int type, void *workspace, int6
 template <int D, int TYPE, int C>
 static int launch_attention_grad_of(const AttentionGradArgs &a, void *stream)
 {
-    if constexpr (D <= 64 && TYPE != TABX_F32) return launch(tabx_attention_grad_kernel<D, TYPE, C>, least(a.works, kMostGroups), 4 * D, a, stream);
-    else return launch(tabx_attention_grad_apart_kernel<D, TYPE, C>, least(3 * a.works, kMostGroups), 4 * D, a, stream);
+    if constexpr (D <= 64 && TYPE != TABX_F32) {
+        return launch(tabx_attention_grad_kernel<D, TYPE, C>, least(a.works, kMostGroups), 4 * D, a, stream);
+    } else {
+        const int64_t groups = least(3 * a.works, kMostGroups);
+        if (a.grad_k && a.grad_state_in && a.grad_state_in == a.grad_state_out && !a.grad_states) {
+            // grad_k's workgroups read the state that grad_v's overwrite: one behind the other
+            AttentionGradArgs before = a, behind = a;
+            before.grad_v = nullptr, before.grad_state_in = nullptr;
+            behind.grad_q = nullptr, behind.grad_k = nullptr;
+            const int rc = launch(tabx_attention_grad_apart_kernel<D, TYPE, C>, groups, 4 * D, before, stream);
+            return rc ? rc : launch(tabx_attention_grad_apart_kernel<D, TYPE, C>, groups, 4 * D, behind, stream);
+        }
+        return launch(tabx_attention_grad_apart_kernel<D, TYPE, C>, groups, 4 * D, a, stream);
+    }
 }
 
 template <int D, int TYPE>

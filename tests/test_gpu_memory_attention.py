@@ -237,6 +237,23 @@ def test_state_in_place_and_on_its_own(B):
     assert want_grad
 
 
+@pytest.mark.parametrize("K,V", [(20, 33), (96, 70)])
+def test_state_gradient_in_place_of_many_heads(B, K, V):
+    """More heads than the machine holds at a time, of one tick: each gradient reads what it is given, whoever is first."""
+    T, R, H = 1, 1501, 3
+    g = on_gpu(make(22, T, R, H, K, V, torch.float32))
+    got = []
+    for in_place in (False, True):
+        given = g["grad_state"].clone()
+        after = given if in_place else torch.empty_like(given)
+        grads = [torch.empty_like(g[n]) for n in ("q", "k", "v")]
+        B.tabx_linear_attention_backward(g["q"], g["k"], g["v"], g["log_decay"], 0.25, g["grad_out"], *grads, g["fresh"], g["state"],
+                                         given, after, workspace(B, T, R, H, K, V))
+        got.append(grads + [after])
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
 def test_no_ticks_and_no_rows(B):
     R, H, K, V = 3, 2, 5, 6
     d = on_gpu(make(12, 1, R, H, K, V, torch.float32))
