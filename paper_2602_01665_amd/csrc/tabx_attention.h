@@ -202,8 +202,15 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// Ticks of a chunk.  Long ones spare steps, short ones room: 64 only where it pays and there are as many.
-constexpr int long_chunk(int d, int type) { return type == TABX_BF16 && d > 32 ? 64 : 32; }
+// Ticks of a chunk.  The state costs as many products a chunk, whatever its length; the ticks among themselves as many as they
+// are long, and longer ones more room.  With 64 and 32 of them, one part each (bf16):
+//   gradients, 64 ticks of 20480 heads of 64, 633 and 675 us; 64 ticks of 5120 heads of 128, 750 and 838;
+//     128 ticks of 40960 heads of 32, 1390 and 1009;
+//   forward, 128 ticks of 20480 heads of 64, 489 and 474; 64 ticks of 20480 heads of 96, 619 and 645; 32768 ticks of 8
+//     heads of 128, 152 and 165; 128 ticks of 81920 heads of 32, 1005 and 925;
+//   segments' states, 8192 ticks of 16 heads of 64, 47.5 and 48.7 with the attention behind them.
+// Operands in several parts have no room for 64.  READS_ONCE: forward.
+constexpr int long_chunk(int d, int type, bool reads_once) { return type == TABX_BF16 && d > (reads_once ? 64 : 32) ? 64 : 32; }
 
 template <int N>
 __device__ __forceinline__ void split(bf16x4 (&part)[N], f32x4 v)
