@@ -93,7 +93,9 @@ struct StepArgs {
 
 // A state is a run of keys x values floats.  LANES lanes have a row's head (64: a whole wavefront); lane l has four
 // consecutive values of every (4 LANES / VALUES)-th line of the state, so that the lanes read and write 16 bytes each of
-// one run.  VALUES: the values, a multiple of four, rounded up to a power of two; lanes beyond the last value idle.
+// one run.  Bound by HBM: the state is read (where it is not forgotten) and written, once each; 1310720 heads of 32 x 32
+// 2.12 ms, 5.1 TB/s; 160000 of 80 x 48 964 us; 96 rows of 4 heads 4.5 us, with the launch 10.8.  Eight lines under way in
+// a lane at a time.  VALUES: the values, a multiple of four, rounded up to a power of two; lanes beyond the last value idle.
 template <int TYPE, int VALUES, int LANES>
 __global__ __launch_bounds__(256) void tabx_attention_step_kernel(const StepArgs a)
 {
@@ -144,7 +146,8 @@ __global__ __launch_bounds__(256) void tabx_attention_step_kernel(const StepArgs
 }
 
 // The same for values that are no multiple of four: a wavefront has a row's head, a lane one value (or two) of every
-// (64 / ACROSS)-th line.
+// (64 / ACROSS)-th line, so that no lane's run goes beyond its line (160000 heads of 33 x 31 in f32 282 us; 527 with runs of
+// four that are asked for their ends).
 template <int TYPE, int ACROSS>
 __global__ __launch_bounds__(256) void tabx_attention_step_odd_kernel(const StepArgs a)
 {
@@ -708,9 +711,9 @@ struct Attention {
     };
 
     // One attention from tick `begin` to `last`; the next chunk's rows are under way while it works on the present one (not
-    // the wide ones', whose registers cost a workgroup of a CU: 810 us with them, 620 without, 128 ticks of 10240 heads of
-    // 128).  READS: queries are answered (else only the state goes on).  part(), course(begin): what to go through, worked
-    // out anew where it is needed.  kept: what is left of the state before.  wild, turn: of the chunk at hand and the one
+    // the wide ones', which have no registers left for them: 128 ticks of 10240 heads of 128 in bf16 2780 us with them, 650
+    // without; of 20480 heads of 64, 489 and 530).  READS: queries are answered (else only the state goes on).  part(),
+    // course(begin): what to go through, worked out anew where it is needed.  kept: what is left of the state before.  wild, turn: of the chunk at hand and the one
     // before, whether not all of it is finite.
     template <bool READS, typename GetPart, typename GetCourse>
     static __device__ __forceinline__ void go_through(State &state, float &kept, In &q, In &k, In &v, Within &within, int (&wild)[2], int &turn,
@@ -814,7 +817,10 @@ __device__ __forceinline__ const Args &again()
     return *(const Args *)p;
 }
 
-// A workgroup goes through its ticks with the state in registers.  CARRY: nothing is read, the states that the segments
+// A workgroup goes through its ticks with the state in registers.  Bound by HBM and by vector instructions next to it, which
+// cut operands into parts and fade them: 128 ticks of 20480 heads of 64 in bf16 461 to 474 us, 4.3 TB/s of q, k, v and out
+// (vector instructions a half of the time, matrix ones a seventh, reads of LDS a third); of 10240 heads of 128 650 us (4.1);
+// in f32 128 ticks of 10240 heads of 64 392 (4.3); 8 ticks of 163840 heads of 64 1158 us (the states: 5.2).  CARRY: nothing is read, the states that the segments
 // would leave of nothing are.
 template <int D, int TYPE, int C, bool CARRY>
 __global__ __launch_bounds__(4 * D, attention_wavefronts(D, TYPE)) void tabx_attention_kernel(const AttentionPair)
@@ -865,7 +871,9 @@ __global__ __launch_bounds__(4 * D, attention_wavefronts(D, TYPE)) void tabx_att
 }
 
 // The gradients: forwards through the ticks for grad_q, then backwards for grad_k and grad_v, which read the same rows,
-// and the state's; the last chunk forwards is the first one backwards, and what was read is still in the caches.
+// and the state's; the last chunk forwards is the first one backwards, and what was read is still in the caches.  Bound by
+// vector instructions (half of the time) beside HBM: 64 ticks of 20480 heads of 64 in bf16 634 us, 3.4 TB/s of seven arrays.
+// The loads of the next chunk do not go ahead here: four arrays of rows would cost a wavefront of a SIMD.
 template <int D, int TYPE, int C>
 __global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tabx_attention_grad_kernel(const AttentionGradArgs)
 {
@@ -873,7 +881,6 @@ __global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tab
     typedef AttentionGradArgs Args;
     typedef typename A::T T;
     constexpr int bytes = sizeof(T);
-    constexpr bool kAhead = false;
     __shared__ typename A::In q, k, v, g;
     __shared__ typename A::Within within;
     __shared__ int wild[2];
@@ -955,10 +962,9 @@ __global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tab
             A::load(vr, b.q, b.q_tick, c, n, b.keys);
             flag = c.begins(lane, n);
         };
-        if (kAhead && begin < last) fetch(begin);
         for (; begin < last; begin += C) {
             const int n = (int)min((int64_t)C, last - begin);
-            if (!kAhead) fetch(begin);
+            fetch(begin);
             float l2 = decay;                      // (as in go_through)
             int col = lane & 15, quad = lane >> 4;
             asm volatile("" : "+v"(l2), "+v"(col), "+v"(quad));
@@ -970,7 +976,6 @@ __global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tab
             const uint32_t odd = A::store(q, qr) | A::store(g, gr);
             if (__ballot(odd != 0) && lane == 0) wild[turn] = 1;
             const uint64_t begins = __ballot(flag != 0);
-            if (kAhead && begin + C < last) fetch(begin + C);
             lds_meet();
             const bool odd_one = wild[turn] != 0;
             if (again<Args>().grad_k) {
@@ -996,7 +1001,9 @@ __global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tab
     }
 }
 
-// The gradients, each by a workgroup of its own: neighbours, which share what they read.
+// The gradients, each by a workgroup of its own: neighbours, which share what they read.  64 ticks of 5120 heads of 128 in
+// bf16 740 us; 100 ticks of 1887 heads of 48 x 80 in f32, half of them controlled, 372 us, most of it waits of one
+// workgroup at a time on a CU for its own steps.
 template <int D, int TYPE, int C>
 __global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tabx_attention_grad_apart_kernel(const AttentionGradArgs)
 {
@@ -1057,7 +1064,9 @@ __global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tab
     }
 }
 
-// The states that the segments leave become those before them, one behind the other: a thread per element.
+// The states that the segments leave become those before them, one behind the other: a thread per element, with 32 segments
+// under way at a time, as a load behind a store into what may be the same array would wait for it (64 segments of 8 states
+// of 128 x 128 13 us).
 static __global__ __launch_bounds__(256) void tabx_attention_join_kernel(const AttentionPair pair)
 {
     const AttentionArgs &a = pair.of[blockIdx.y];

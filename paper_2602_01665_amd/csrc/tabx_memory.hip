@@ -21,9 +21,19 @@ namespace tabx {
 
 // --- root-mean-square norm ----------------------------------------------------------------------
 
-constexpr int64_t kRmsTeams = 10 * 8192;           // teams that share the rows of a forward call, if they are many
-constexpr int64_t kRmsTurns = 4;                   // turns of a team's run of rows in a backward call
-constexpr int64_t kRmsAlone = 2;                   // workgroups whose rows one takes alone in a backward call
+// Teams that share the rows of a forward call, if they are many (327680 rows of 512: 118 us, 134 with 8192), turns of a team's
+// run of rows in a backward call (42517 rows of 1000: 88 us, 105 with 32), and of how many workgroups one takes the rows
+// alone in a backward call, whose sums are then the gradient (32 rows of 1000: 9.5 us, 12.2 with two and a joining launch; 96
+// rows 17.3 alone, 12.6 with six).
+constexpr int64_t kRmsTeams = 10 * 8192;
+constexpr int64_t kRmsTurns = 4;
+constexpr int64_t kRmsAlone = 2;
+
+// Whether the pieces of a row that sixteen lanes store lie across lines.
+static bool across_lines(const void *data, int64_t stride, int type)
+{
+    return data && type != TABX_F32 && !(on_boundary(data, 64) && stride * size_of(type) % 64 == 0);
+}
 
 template <int LANES, int PIECES>
 struct RmsForward {
@@ -43,6 +53,11 @@ struct RmsForward {
         a.team_rows = LANES <= 64 ? least(quotient_up(quotient_up(a.rows, kRmsTeams), at_once(LANES)) * at_once(LANES), 64) : 1;
         const int64_t groups = least(quotient_up(a.rows, a.team_rows * teams), stays ? kComputeUnits * 2048 / LANES : kMostGroups);
         a.lap = groups * teams * a.team_rows;
+        // what the L2s would not hold goes past them (327680 rows of 512, half of them, bf16 and e4m3, 118 us, 112; all of
+        // them in bf16 234, 225), but for pieces of lines, as in the layer norm
+        const bool across = LANES == 16 && PIECES > 1 && (across_lines(a.sum, a.sum_stride, a.sum_type) || across_lines(a.y, a.y_stride, a.y_type));
+        const int64_t written = a.rows * a.width * ((a.sum ? size_of(a.sum_type) : 0) + size_of(a.y_type));
+        a.stream = !across && written > kL2Bytes;
         return a.x_type == TABX_F32 ? with_type<4>(a, groups, stream) : with_type<2>(a, groups, stream);
     }
 };
@@ -190,7 +205,8 @@ static int rotary_in_runs(RotaryArgs a, bool interleaved, bool copies, void *str
 
 static int rotary(const RotaryArgs &a, int type, bool interleaved, bool copies, void *stream)
 {
-    const bool eight = a.pairs % 8 == 0 && a.width % 8 == 0;       // 16 bytes of 16-bit elements
+    // 16 bytes of 16-bit elements (327680 rows of 8 heads of 64: 143 us, 154 with runs of four)
+    const bool eight = a.pairs % 8 == 0 && a.width % 8 == 0;
     if (type == TABX_F32) return rotary_in_runs<TABX_F32, 4>(a, interleaved, copies, stream);
     if (type == TABX_BF16) return eight ? rotary_in_runs<TABX_BF16, 8>(a, interleaved, copies, stream) : rotary_in_runs<TABX_BF16, 4>(a, interleaved, copies, stream);
     return eight ? rotary_in_runs<TABX_F16, 8>(a, interleaved, copies, stream) : rotary_in_runs<TABX_F16, 4>(a, interleaved, copies, stream);
@@ -215,7 +231,9 @@ static int form_width(int32_t keys, int32_t values)
 }
 
 // Into how many segments of how many ticks a row's ticks are cut: where there are few rows and heads, so many that every
-// CU has the workgroups that it holds, each of some chunks.
+// CU has the workgroups that it holds, each of some chunks.  At least 64 ticks: 1024 ticks of 8 heads of 64 take 20 us,
+// their gradients 31; with 128 at least 25 and 43, with 256 36 and 69.  Half as many workgroups: 32768 ticks of 8 heads of
+// 128 190 us instead of 152, gradients of 512 ticks of 80 heads of 64 59 instead of 53 (of 8192 ticks of 16, 96 instead of 103).
 struct Segments {
     int64_t count, ticks;
 };
@@ -256,6 +274,7 @@ static int launch_attention_of(const AttentionPair &pair, int count, void *strea
     constexpr int chunk = long_chunk(D, TYPE, !CARRY);
     const int64_t groups = least(pair.of[0].works, kMostGroups);
     if constexpr (chunk > 32 && !CARRY)            // (no segments are that short)
+        // (8 ticks of 163840 heads of 64 were 1665 us in a chunk of 64, half empty, and are 1158)
         if (pair.of[0].ticks <= 32) return launch_pair(tabx_attention_kernel<D, TYPE, 32, CARRY>, groups, 4 * D, pair, count, stream);
     return launch_pair(tabx_attention_kernel<D, TYPE, chunk, CARRY>, groups, 4 * D, pair, count, stream);
 }
@@ -291,6 +310,10 @@ static int carry(AttentionPair &pair, int count, int type, void *workspace, int6
     return launch_pair(tabx_attention_join_kernel, least(quotient_up(a.rows * a.heads * a.keys * a.values, 256), kMostGroups), 256, pair, count, stream);
 }
 
+// 16-bit operands of up to 64: one workgroup for all three gradients, which reads everything once where three would twice
+// (64 ticks of 20480 heads of 64 634 us, 760 apart; 128 ticks of 40960 heads of 32 1009 and 1093).  Wider or in three parts its
+// two states and four tiles cost more workgroups of a CU than they spare (64 ticks of 5120 heads of 128 957 us, 740 apart; f32,
+// 10240 heads of 64, 639 and 573).
 template <int D, int TYPE, int C>
 static int launch_attention_grad_of(const AttentionGradArgs &a, void *stream)
 {
@@ -340,7 +363,7 @@ static int launch_step(const StepArgs &a, void *stream)
     return launch(tabx_attention_step_kernel<TYPE, VALUES, LANES>, least(quotient_up(a.works, 256 / LANES), kMostGroups), 256, a, stream);
 }
 
-// States of few elements share a wavefront.
+// States of few elements share a wavefront (2621440 of 16 x 16: 1063 us, 2645 with a wavefront each).
 template <int TYPE>
 static int attention_step(const StepArgs &a, void *stream)
 {
