@@ -226,6 +226,10 @@ __global__ __launch_bounds__(threads_of(LANES), grad_wavefronts(PIECES)) void ta
                 g[q] *= w[q];
                 if (q < PIECES - 1) along = fma4(g[q], x[q], along);
             }
+            if constexpr (STREAMED && LANES > 64) {    // (grad_x may lie where grad_sum does, and several wavefronts read a
+#pragma unroll                                         // row's last elements: all of them have theirs before the first store)
+                for (int q = 0; q < PIECES; ++q) asm volatile("" ::"v"(h.s.v[q]) : "memory");
+            }
             const float sh = row_sum<LANES>(sum_of(along), slots[turn]) * a.inv_width;
             turn ^= 1;
 #pragma unroll

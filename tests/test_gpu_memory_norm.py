@@ -201,3 +201,21 @@ def test_large_calls_are_the_small_ones(B):
             B.tabx_rms_norm(x[c], None, EPS, y1, sc1, r1, residual[c], s1, mask[c])
             for a, b in ((s, s1), (y.view(torch.uint8), y1.view(torch.uint8)), (scale, sc1), (rstd, r1)):
                 assert torch.equal(a[c], b)
+
+
+@pytest.mark.parametrize("W", [1025, 1030, 1537, 2049, 2050, 3071, 4093, 4097, 8190])
+def test_gradient_in_the_streams_place_of_wide_rows(B, W):
+    """Rows that several wavefronts share: the last elements, which more than one of them reads, are read before they are
+    overwritten; bit for bit what a call with an output of its own gives."""
+    g = torch.Generator("cuda").manual_seed(W)
+    R = 1500
+    for t in (F32, BF16):
+        s, gy, gs = (torch.randn(R, W, generator=g, device="cuda").to(t) for _ in range(3))
+        rstd = torch.rsqrt((s.float() ** 2).mean(1) + EPS)
+        apart, together = torch.full_like(s, 7.0), gs.clone()
+        B.tabx_rms_norm_backward(s, None, rstd, gy, gs, apart)
+        B.tabx_rms_norm_backward(s, None, rstd, gy, together, together)
+        assert torch.equal(apart, together), t
+        some = torch.arange(0, R, 97)
+        want = M.norm_grad(s.cpu()[some], None, rstd.cpu()[some], gy.cpu()[some], gs.cpu()[some], torch.ones(len(some), dtype=torch.bool), t, 1)
+        M.near(together.cpu()[some], *want["grad_x"], t)

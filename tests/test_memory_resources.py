@@ -56,3 +56,25 @@ def test_arguments_are_not_spilled(listing):
     for name, meta in re.findall(r"\.name:\s+(_ZN4tabx\d+tabx_attention_\w+)\n(.*?)\.wavefront_size", listing, re.S):
         spilled = int(re.search(r"\.sgpr_spill_count:\s+(\d+)", meta)[1])
         assert spilled <= 64, (name, spilled)
+
+
+def test_a_stream_gradient_in_place_is_read_before_it_is_overwritten(listing):
+    """A row of more lanes than a wavefront has its last elements read by several of them, and grad_x may lie where
+    grad_sum does: behind the barrier of a row's sum, at whose other side stores begin, only the next row's loads (of the
+    widest form: rstd and three arrays) may be under way."""
+    seen = 0
+    for m in re.finditer(r"^(_ZN4tabx\w*rms_grad_kernelI\w+):.*?\n(.*?)s_endpgm", listing, re.S | re.M):
+        lanes, pieces, *_, streamed = map(int, re.search(r"ILi(\d+)ELi(\d+)ELi(\d)ELi(\d)ELb(\d)ELb(\d)", m[1]).groups())
+        if lanes <= 64 or not streamed:
+            continue
+        seen += 1
+        under_way = 1 + 3 * pieces if lanes == 1024 else 0
+        sums, waited = 0, None
+        for line in m[2].split("\n"):
+            w = re.match(r"\s*s_waitcnt.*vmcnt\((\d+)\)", line)
+            waited = int(w[1]) if w else waited
+            if re.match(r"\s*s_barrier", line) and waited is not None:
+                sums += 1
+                assert waited <= under_way, (m[1], waited)
+        assert sums, m[1]
+    assert seen == 20
