@@ -621,7 +621,10 @@ int tabx_linear_attention_step(int64_t rows, int32_t heads, int32_t key_width, i
                                const TabxHeads *out, void *stream);
 
 /* Many ticks at once, from state_in (NULL: zero; not written) to state_out (NULL: not wanted; may be
- * state_in).  No ticks: state_out is state_in, or zero.  The same sums as the steps' in another order.
+ * state_in).  No ticks: state_out is state_in, or zero.  The same sums as the steps' in another order, in 32
+ * bits; but of bf16 arrays the products q_t k_s of two ticks, and the state where it is read (not where it is
+ * kept), are rounded to 16 bits on the way to out and to the gradients: each is off by up to 2^-17 of the
+ * magnitudes of its terms, beside its own rounding to bf16 (2^-8 of itself).
  * `workspace`: device memory, 16-byte aligned, of at least tabx_linear_attention_workspace() bytes
  * (TABX_ERR_SHAPE if workspace_bytes is less; may be NULL if that is 0), whose contents need no
  * preparation; calls (and replays of captured graphs) that may run at the same time need one each. */

@@ -191,14 +191,16 @@ __global__ __launch_bounds__(256) void tabx_attention_step_odd_kernel(const Step
 // --- many ticks ---------------------------------------------------------------------------------
 
 // The products run in the matrix cores in bf16 with sums in 32 bits, where every 32-bit operand stands as the sum of parts
-// of 8 bits each: bf16 inputs are one part, f16 ones two (both exact), f32 ones three; what lies between on the way to an
-// output (the products of queries and keys, the state) is cut into two parts, three for f32, so that 2^-16 of a term is lost,
-// 2^-23 for f32, where the output's own rounding is 2^-8, 2^-11, 2^-24; what goes into the state, which is kept in 32 bits,
-// always into three.  Of the parts' products those are taken that are above the last part's rounding.  Nothing leaves the
-// range of 32 bits that 32 bits would hold.
+// of 8 bits each: bf16 inputs are one part, f16 ones two (both exact), f32 ones three; what goes into the state, which is kept
+// in 32 bits, is cut into three.  So is what lies between on the way to an output (the products of queries and keys, the
+// state that is read) for f16 and f32, and of the parts' products those are left out that are below 2^-24 of a term.  For
+// bf16 it is cut into two, which round it to 16 bits: 2^-17 of a term, where the output's own rounding is 2^-8 of the result.
+// (A third one there: 128 ticks of 20480 heads of 64 502 us instead of 476, 64 ticks of 20480 heads of 96 844 instead of 622,
+// gradients of 64 ticks of 20480 heads of 64 719 instead of 639, of 5120 heads of 128 860 instead of 750.  For f16, whose
+// rounding is 2^-11, two and without the product of two second parts: 128 ticks of 20480 heads of 64 519 instead of 570.)
 template <int TYPE> struct Parts {
     static constexpr int in = TYPE == TABX_BF16 ? 1 : TYPE == TABX_F16 ? 2 : 3;
-    static constexpr int mid = TYPE == TABX_F32 ? 3 : 2;
+    static constexpr int mid = TYPE == TABX_BF16 ? 2 : 3;
 };
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -227,11 +229,12 @@ __device__ __forceinline__ void split(bf16x4 (&part)[N], f32x4 v)
 
 __device__ __forceinline__ bf16x8 join(bf16x4 a, bf16x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 
-// One product of operands in parts, the smallest parts' first.
+// One product of operands in parts, the smallest parts' first: those of three parts whose places in their operands add up to
+// less than three, all of two.
 template <int NA, int NB>
 __device__ __forceinline__ f32x4 multiply(const bf16x8 (&a)[NA], const bf16x8 (&b)[NB], f32x4 c)
 {
-    constexpr int last = NA > NB ? NA : NB;
+    constexpr int last = NA + NB - 1 < 3 ? NA + NB - 1 : 3;
 #pragma unroll
     for (int s = last - 1; s >= 0; --s)
 #pragma unroll
@@ -499,14 +502,35 @@ struct Attention {
 #pragma unroll
         for (int b = 0; b < C / 32; ++b) v.across(values[b], 32 * b, 16 * wave, col, quad);
         if constexpr (READS) {
-            bf16x8 held[D / 32][MID];
-#pragma unroll
-            for (int s = 0; s < D / 32; ++s) {
+            // the state as operands, all of it at a time, or (IN_TURN: it would not fit the registers) 32 lines after the other
+            constexpr bool IN_TURN = D >= 96 && MID == 3 && IN == 2;
+            bf16x8 held[IN_TURN ? 1 : D / 32][MID];
+            f32x4 read[IN_TURN ? C / 16 : 1];
+            const auto hold = [&](bf16x8(&operand)[MID], int s) {
                 bf16x4 x[MID], y[MID];
                 split(x, state[2 * s]);
                 split(y, state[2 * s + 1]);
 #pragma unroll
-                for (int m = 0; m < MID; ++m) held[s][m] = join(x[m], y[m]);
+                for (int m = 0; m < MID; ++m) operand[m] = join(x[m], y[m]);
+            };
+            if constexpr (IN_TURN) {
+#pragma unroll
+                for (int I = 0; I < C / 16; ++I) read[I] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int s = 0; s < D / 32; ++s) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    hold(held[0], s);
+#pragma unroll
+                    for (int I = 0; I < C / 16; ++I) {
+                        if (16 * I >= n) continue;
+                        bf16x8 x[IN];
+                        q.along_results(x, 16 * I, 32 * s, col, quad);
+                        read[I] = multiply(held[0], x, read[I]);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int s = 0; s < D / 32; ++s) hold(held[s], s);
             }
             const int d = 16 * wave + 4 * quad;
             int64_t tick = a.out_tick;
@@ -519,11 +543,15 @@ struct Attention {
                 __builtin_amdgcn_sched_barrier(0); // (operands of all of them at a time would not fit)
                 const int i = 16 * I + col;
                 f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+                if constexpr (IN_TURN) {
+                    o = read[I];
+                } else {
 #pragma unroll
-                for (int s = 0; s < D / 32; ++s) {
-                    bf16x8 x[IN];
-                    q.along_results(x, 16 * I, 32 * s, col, quad);
-                    o = multiply(held[s], x, o);
+                    for (int s = 0; s < D / 32; ++s) {
+                        bf16x8 x[IN];
+                        q.along_results(x, 16 * I, 32 * s, col, quad);
+                        o = multiply(held[s], x, o);
+                    }
                 }
                 const float fade = __builtin_amdgcn_exp2f(l2 * (float)(i + 1 - a.backward)) * a.scale_read;
                 o *= fade;
@@ -804,7 +832,7 @@ struct Work {
 
 // Wavefronts of a SIMD, as many as the LDS of a workgroup lets the machine hold.
 constexpr int attention_wavefronts(int d, int type) { return d >= 96 ? type == TABX_F32 ? 2 : 4 : 3; }
-constexpr int attention_grad_wavefronts(int d, int type) { return d <= 64 ? 3 : type == TABX_F32 ? 2 : d == 128 && type == TABX_F16 ? 3 : 4; }
+constexpr int attention_grad_wavefronts(int d, int type) { return d <= 64 ? 3 : type == TABX_F32 ? 2 : 4; }
 
 // The launch arguments, fetched anew for what follows.  A wavefront has too few scalar registers for what all of a kernel
 // needs, and what is fetched once at the top is spilled to vector registers (a quarter of the gradients' instructions).
