@@ -625,6 +625,9 @@ int tabx_linear_attention_step(int64_t rows, int32_t heads, int32_t key_width, i
  * bits; but of bf16 arrays the products q_t k_s of two ticks, and the state where it is read (not where it is
  * kept), are rounded to 16 bits on the way to out and to the gradients: each is off by up to 2^-17 of the
  * magnitudes of its terms, beside its own rounding to bf16 (2^-8 of itself).
+ * Elements of 2^30 and more, a state of 2^70 and more, a scale above 2^16 and what is not finite are taken
+ * tick by tick, which is slower, so that no sum leaves 32 bits that the steps hold in them.  At the lower end
+ * a product of two elements, or what the decay leaves between two ticks, may count as zero below 2^-126.
  * `workspace`: device memory, 16-byte aligned, of at least tabx_linear_attention_workspace() bytes
  * (TABX_ERR_SHAPE if workspace_bytes is less; may be NULL if that is 0), whose contents need no
  * preparation; calls (and replays of captured graphs) that may run at the same time need one each. */

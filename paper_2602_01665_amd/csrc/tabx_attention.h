@@ -40,6 +40,7 @@ struct AttentionArgs {
     int64_t     segment;           // ticks of a segment, a multiple of the chunk
     int32_t     segments, heads, units, keys, values;
     int32_t     backward;          // in time
+    int32_t     exactly;           // the scale is beyond kMostScale
     float       scale_read, scale_added;   // of what is read, of what is taken in
 };
 
@@ -60,6 +61,7 @@ struct AttentionGradArgs {
     const float *states, *grad_states;     // before each segment, forwards and backwards in time, or nullptr
     int64_t     ticks, rows, envs, works, segment;
     int32_t     segments, heads, units, keys, values;
+    int32_t     exactly;           // the scale is beyond kMostScale
     float       scale;
 };
 
@@ -274,18 +276,28 @@ struct Eight {
     }
 };
 
-// Not 0 in a bit of its own if one of them is not finite (an exponent of ones carries), or, of 32 bits, so large that its
-// first part would not be.
+// Up to where products of matrices take the place of the recurrence's own order, in which less may pass 32 bits: q, k and v below
+// 2^30, a scale of at most 2^16, a state below 2^70 before the first of 64 chunks (kSmallChunks).  Then with keys and values of
+// 2^7 at most and chunks of 2^6 ticks
+//   |q k scale| < 2^(7 + 30 + 30 + 16),  sum over keys' ticks |q k scale v| < 2^(83 + 6 + 30) = 2^119,
+//   |S| < 2^70 + 2^(12 + 30 + 30 + 16) < 2^89 (scaled as it is taken in; else the 16 stand at its reading),  |q S scale| < 2^126,
+// and every part, every sum in any order is finite.  What lies beyond goes through the chunk tick by tick.
+// (To look costs 1 % of the time: 128 ticks of 20480 heads of 64 474 us, 477; gradients of 64 ticks of them 636, 643.)
+constexpr float kMostScale = 0x1p16f, kLargeState = 0x1p70f;
+constexpr int kSmallChunks = 64;
+
+// Not 0 in a bit of its own if one of them is 2^30 or more (an exponent of at least that many carries) or not finite; values
+// of f16 end below that.
 template <int TYPE>
-__device__ __forceinline__ uint32_t not_finite(const Eight<TYPE> &e)
+__device__ __forceinline__ uint32_t beyond(const Eight<TYPE> &e)
 {
     constexpr uint32_t exponent = TYPE == TABX_F32 ? 0x7f800000u : TYPE == TABX_BF16 ? 0x7f807f80u : 0x7c007c00u;
-    constexpr uint32_t one = TYPE == TABX_F32 ? 0x01000000u : TYPE == TABX_BF16 ? 0x00800080u : 0x04000400u;
+    constexpr uint32_t rest = TYPE == TABX_F32 ? 0x31800000u : TYPE == TABX_BF16 ? 0x31803180u : 0x04000400u;
     uint32_t found = 0;
 #pragma unroll
     for (int n = 0; n < (TYPE == TABX_F32 ? 2 : 1); ++n)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) found |= (e.v[n][i] & exponent) + one;
+        for (int i = 0; i < 4; ++i) found |= (e.v[n][i] & exponent) + rest;
     return found & (TYPE == TABX_F32 ? 0x80000000u : 0x80008000u);
 }
 
@@ -360,7 +372,7 @@ struct Part {
     const void *q, *k, *v;
     void       *out;               // or nullptr
     int64_t     q_tick, k_tick, v_tick, out_tick;
-    int         keys, values, backward;
+    int         keys, values, backward, exactly;
     float       scale_read, scale_added;
 };
 
@@ -443,7 +455,7 @@ struct Attention {
 #pragma unroll
         for (int p = 0; p < PASSES; ++p) {
             tile.template put<TYPE>(p * (THREADS / across) + (int)threadIdx.x / across, 8 * ((int)threadIdx.x % across), rows.e[p]);
-            found |= not_finite<TYPE>(rows.e[p]);
+            found |= beyond<TYPE>(rows.e[p]);
         }
         return found;
     }
@@ -632,8 +644,8 @@ struct Attention {
         }
     }
 
-    // The same for a chunk with keys or values that are not finite, tick by tick: in a product of matrices they would reach
-    // ticks that they do not belong to, as zero times them is not zero.
+    // The same for a chunk with elements that are not finite, tick by tick: in a product of matrices they would reach ticks that
+    // they do not belong to, as zero times them is not zero; and for what may pass 32 bits there and not here (kMostScale).
     template <bool READS>
     static __device__ __forceinline__ void advance_slowly(State &state, uint64_t begins, int n, float l2, const Part &a, const Course &c, int wave, int col, int quad)
     {
@@ -728,6 +740,15 @@ struct Attention {
         for (int s = 0; s < TILES; ++s) state[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
+    // Whether a lane's part of a state is too large for products of matrices.  (NaN is not: it stays in its element there.)
+    static __device__ __forceinline__ bool large(const State &state)
+    {
+        float most = 0.0f;
+#pragma unroll
+        for (int s = 0; s < TILES; ++s) most = fmaxf(most, fmaxf(fmaxf(fabsf(state[s].x), fabsf(state[s].y)), fmaxf(fabsf(state[s].z), fabsf(state[s].w))));
+        return most >= kLargeState;
+    }
+
     // What the decay leaves in 0 to 3 ticks.
     struct Powers {
         float of[4];
@@ -742,14 +763,14 @@ struct Attention {
     // the wide ones', which have no registers left for them: 128 ticks of 10240 heads of 128 in bf16 2780 us with them, 650
     // without; of 20480 heads of 64, 489 and 530).  READS: queries are answered (else only the state goes on).  part(),
     // course(begin): what to go through, worked out anew where it is needed.  kept: what is left of the state before.  wild, turn: of the chunk at hand and the one
-    // before, whether not all of it is finite.
+    // before, whether it goes tick by tick.
     template <bool READS, typename GetPart, typename GetCourse>
     static __device__ __forceinline__ void go_through(State &state, float &kept, In &q, In &k, In &v, Within &within, int (&wild)[2], int &turn,
                                                       GetPart part, GetCourse course, int64_t begin, int64_t last, float decay)
     {
         const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
         Rows qr, kr, vr;
-        int flag = 0;
+        int flag = 0, small = 0;                   // small: chunks for which the state is known to be
         const auto fetch = [&](int64_t from) {
             const Part a = part();
             const Course c = course(from);
@@ -768,10 +789,11 @@ struct Attention {
             int col = lane & 15, quad = lane >> 4;
             asm volatile("" : "+v"(l2), "+v"(col), "+v"(quad));
             turn ^= 1;
-            if (threadIdx.x == 0) wild[turn] = 0;
+            if (threadIdx.x == 0) wild[turn] = part().exactly;
             lds_meet();                                   // the chunk before has been worked on
-            if constexpr (READS) store(q, qr);
-            const uint32_t odd = store(k, kr) | store(v, vr);
+            uint32_t odd = store(k, kr) | store(v, vr);
+            if constexpr (READS) odd |= store(q, qr);
+            if (READS && small == 0) odd |= large(state);
             if (__ballot(odd != 0) && lane == 0) wild[turn] = 1;
             const uint64_t begins = __ballot(flag != 0);       // bit i: an episode begins with the chunk's tick i
             if (kAhead && begin + C < last) fetch(begin + C);
@@ -791,6 +813,7 @@ struct Attention {
                     kr.arrive(), vr.arrive();
                     asm volatile("" : "+v"(flag));
                 });
+            if constexpr (READS) small = __builtin_amdgcn_readfirstlane(wild[turn]) ? 0 : (small == 0 ? kSmallChunks : small) - 1;
             kept = begins || kept < 0.0f ? -1.0f : kept * __builtin_amdgcn_exp2f(l2 * (float)n);
         }
     }
@@ -866,7 +889,7 @@ __global__ __launch_bounds__(4 * D, attention_wavefronts(D, TYPE)) void tabx_att
             constexpr int bytes = sizeof(typename A::T);
             return Part{moved_on(a.q, w.of(a.qs), bytes), moved_on(a.k, w.of(a.ks), bytes), moved_on(a.v, w.of(a.vs), bytes),
                         a.out ? moved_on(a.out, w.of(a.os), bytes) : nullptr, a.qs.tick, a.ks.tick, a.vs.tick, a.os.tick, a.keys, a.values,
-                        a.backward, a.scale_read, a.scale_added};
+                        a.backward, a.exactly, a.scale_read, a.scale_added};
         };
         const auto course = [&](int64_t begin) {
             const AttentionArgs &a = mine();
@@ -942,7 +965,7 @@ __global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tab
                 const auto part = [&] {
                     const Args &a = again<Args>();
                     return Part{moved_on(a.grad_out, w.of(a.os), bytes), moved_on(a.v, w.of(a.vs), bytes), moved_on(a.k, w.of(a.ks), bytes),
-                                moved_on(a.grad_q, w.of(a.gqs), bytes), a.os.tick, a.vs.tick, a.ks.tick, a.gqs.tick, a.values, a.keys, 0, a.scale, 1.0f};
+                                moved_on(a.grad_q, w.of(a.gqs), bytes), a.os.tick, a.vs.tick, a.ks.tick, a.gqs.tick, a.values, a.keys, 0, a.exactly, a.scale, 1.0f};
                 };
                 A::template go_through<true>(state, kept, g, v, k, within, wild, turn, part, [&](int64_t begin) { return course(begin, 0); }, first, last, decay);
             }
@@ -969,16 +992,16 @@ __global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tab
         const auto to_k = [&] {
             const Args &a = again<Args>();
             return Part{moved_on(a.v, w.of(a.vs), bytes), moved_on(a.grad_out, w.of(a.os), bytes), moved_on(a.q, w.of(a.qs), bytes),
-                        moved_on(a.grad_k, w.of(a.gks), bytes), a.vs.tick, a.os.tick, a.qs.tick, a.gks.tick, a.values, a.keys, 1, 1.0f, a.scale};
+                        moved_on(a.grad_k, w.of(a.gks), bytes), a.vs.tick, a.os.tick, a.qs.tick, a.gks.tick, a.values, a.keys, 1, a.exactly, 1.0f, a.scale};
         };
         const auto to_v = [&] {
             const Args &a = again<Args>();
             return Part{moved_on(a.k, w.of(a.ks), bytes), moved_on(a.q, w.of(a.qs), bytes), moved_on(a.grad_out, w.of(a.os), bytes),
                         a.grad_v ? moved_on(a.grad_v, w.of(a.gvs), bytes) : nullptr, a.ks.tick, a.qs.tick, a.os.tick, a.gvs.tick, a.keys, a.values,
-                        1, 1.0f, a.scale};
+                        1, a.exactly, 1.0f, a.scale};
         };
         typename A::Rows qr, kr, vr, gr;
-        int flag = 0;
+        int flag = 0, small = 0;                   // (as in go_through, of both states)
         const auto fetch = [&](int64_t from) {
             const Course c = course(from, 1);
             const int n = (int)min((int64_t)C, last - from);
@@ -997,11 +1020,11 @@ __global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tab
             int col = lane & 15, quad = lane >> 4;
             asm volatile("" : "+v"(l2), "+v"(col), "+v"(quad));
             turn ^= 1;
-            if (threadIdx.x == 0) wild[turn] = 0;
+            if (threadIdx.x == 0) wild[turn] = again<Args>().exactly;
             lds_meet();
-            A::store(k, kr);
+            uint32_t odd = A::store(k, kr) | A::store(q, qr) | A::store(g, gr);
             A::store(v, vr);
-            const uint32_t odd = A::store(q, qr) | A::store(g, gr);
+            if (small == 0) odd |= (uint32_t)A::large(turned) | (uint32_t)A::large(state);
             if (__ballot(odd != 0) && lane == 0) wild[turn] = 1;
             const uint64_t begins = __ballot(flag != 0);
             lds_meet();
@@ -1021,6 +1044,7 @@ __global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tab
             const Course c = course(begin, 1);
             if (__builtin_expect(odd_one, 0)) A::template advance_slowly<true>(state, begins, n, l2, a, c, wave, col, quad);
             else A::template advance<true>(state, within, k, q, g, begins, n, l2, a, c, wave, col, quad, [] {});
+            small = __builtin_amdgcn_readfirstlane(odd_one) ? 0 : (small == 0 ? kSmallChunks : small) - 1;
         }
         // what is left for the state before the first tick, if that belongs to its episode
         const Args &a = again<Args>();
@@ -1054,9 +1078,9 @@ __global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tab
             const Args &a = again<Args>();
             const void *const xq = moved_on(a.q, w.of(a.qs), bytes), *const xk = moved_on(a.k, w.of(a.ks), bytes),
                               *const xv = moved_on(a.v, w.of(a.vs), bytes), *const xg = moved_on(a.grad_out, w.of(a.os), bytes);
-            if (role == 0) return Part{xg, xv, xk, moved_on(a.grad_q, w.of(a.gqs), bytes), a.os.tick, a.vs.tick, a.ks.tick, a.gqs.tick, a.values, a.keys, 0, a.scale, 1.0f};
-            if (role == 1) return Part{xv, xg, xq, moved_on(a.grad_k, w.of(a.gks), bytes), a.vs.tick, a.os.tick, a.qs.tick, a.gks.tick, a.values, a.keys, 1, 1.0f, a.scale};
-            return Part{xk, xq, xg, a.grad_v ? moved_on(a.grad_v, w.of(a.gvs), bytes) : nullptr, a.ks.tick, a.qs.tick, a.os.tick, a.gvs.tick, a.keys, a.values, 1, 1.0f, a.scale};
+            if (role == 0) return Part{xg, xv, xk, moved_on(a.grad_q, w.of(a.gqs), bytes), a.os.tick, a.vs.tick, a.ks.tick, a.gqs.tick, a.values, a.keys, 0, a.exactly, a.scale, 1.0f};
+            if (role == 1) return Part{xv, xg, xq, moved_on(a.grad_k, w.of(a.gks), bytes), a.vs.tick, a.os.tick, a.qs.tick, a.gks.tick, a.values, a.keys, 1, a.exactly, 1.0f, a.scale};
+            return Part{xk, xq, xg, a.grad_v ? moved_on(a.grad_v, w.of(a.gvs), bytes) : nullptr, a.ks.tick, a.qs.tick, a.os.tick, a.gvs.tick, a.keys, a.values, 1, a.exactly, 1.0f, a.scale};
         };
         const auto course = [&](int64_t begin) {
             const Args &a = again<Args>();

@@ -553,7 +553,7 @@ int tabx_linear_attention(int64_t ticks, int64_t rows, int32_t heads, int32_t ke
     a.state_in = state_in, a.state_out = state_out;
     a.ticks = ticks, a.rows = rows, a.envs = rows / units, a.works = rows * heads * s.count, a.segment = s.ticks;
     a.segments = (int32_t)s.count, a.heads = heads, a.units = units, a.keys = key_width, a.values = value_width;
-    a.scale_read = scale, a.scale_added = 1.0f;
+    a.exactly = !(fabsf(scale) <= kMostScale), a.scale_read = scale, a.scale_added = 1.0f;
     AttentionPair pair = {{a}};
     if (s.count > 1 && (rc = carry(pair, 1, type, workspace, 0, stream))) return rc;
     return attention_of_width<false>(pair, 1, type, stream);
@@ -600,7 +600,7 @@ int tabx_linear_attention_backward(int64_t ticks, int64_t rows, int32_t heads, i
     a.state_in = state_in, a.grad_state_out = grad_state_out, a.grad_state_in = grad_state_in;
     a.ticks = ticks, a.rows = rows, a.envs = rows / units, a.works = rows * heads * s.count, a.segment = s.ticks;
     a.segments = (int32_t)s.count, a.heads = heads, a.units = units, a.keys = key_width, a.values = value_width;
-    a.scale = scale;
+    a.exactly = !(fabsf(scale) <= kMostScale), a.scale = scale;
     if (s.count > 1) {
         AttentionArgs c = {};
         c.log_decay = log_decay, c.fresh = fresh, c.controlled = controlled;
@@ -615,7 +615,7 @@ int tabx_linear_attention_backward(int64_t ticks, int64_t rows, int32_t heads, i
         }
         if (grad_k || grad_v || grad_state_in) {
             c.k = a.q, c.v = a.grad_out, c.ks = a.qs, c.vs = a.os;
-            c.state_in = grad_state_out, c.scale_added = scale, c.backward = 1;
+            c.state_in = grad_state_out, c.scale_added = scale, c.exactly = a.exactly, c.backward = 1;
             pair.of[count++] = c;
         }
         if ((rc = carry(pair, count, type, workspace, carried_bytes(s, rows, heads, key_width, value_width), stream))) return rc;
