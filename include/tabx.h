@@ -610,7 +610,8 @@ int tabx_rotary(int64_t rows, int32_t heads, int32_t width, const TabxHeads *x,
  *   states are [rows][heads][key_width][value_width] f32, without gaps.
  * scale is finite (TABX_ERR_PARAM).  1 <= heads <= TABX_ATTENTION_MAX_HEADS, rows * heads <= 2^31 - 1, ticks <= 2^30,
  * 1 <= key_width, value_width <= TABX_ATTENTION_MAX_WIDTH (TABX_ERR_SHAPE).  No rows: nothing to do.
- * A value that is not finite reaches its own head from its tick on, until an episode ends.
+ * What is not finite reaches what these sums have it in, of its own head and row, from its tick on until an
+ * episode ends, and nothing else.
  *
  * tabx_linear_attention_step: one tick of a rollout (strides of ticks are not looked at; fresh [rows / units],
  * normally `dones` as the tick call before it left them).  `state` is updated where it lies. */
@@ -650,7 +651,8 @@ int64_t tabx_linear_attention_workspace(int64_t ticks, int64_t rows, int32_t hea
  *   grad_state_in = e_h D_0 (0 where tick 0 is the first of an episode).
  * log_decay is a setting and has no gradient.  All of the arrays are of one type.  Rows that are not
  * controlled have gradients of zero, and nothing of them is read.  grad_state_in may be grad_state_out.
- * A value that is not finite may reach the gradients of other ticks of its row and head, in any episode. */
+ * What is not finite reaches what these sums have it in, of its own head and row and within its episode
+ * (grad_q of its tick and later ones, grad_k and grad_v of its tick and earlier ones), and nothing else. */
 int tabx_linear_attention_backward(int64_t ticks, int64_t rows, int32_t heads, int32_t key_width,
                                    int32_t value_width, const TabxHeads *q, const TabxHeads *k,
                                    const TabxHeads *v, const float *log_decay, float scale,

@@ -282,7 +282,7 @@ struct Eight {
 //   |q k scale| < 2^(7 + 30 + 30 + 16),  sum over keys' ticks |q k scale v| < 2^(83 + 6 + 30) = 2^119,
 //   |S| < 2^70 + 2^(12 + 30 + 30 + 16) < 2^89 (scaled as it is taken in; else the 16 stand at its reading),  |q S scale| < 2^126,
 // and every part, every sum in any order is finite.  What lies beyond goes through the chunk tick by tick.
-// (To look costs 1 % of the time: 128 ticks of 20480 heads of 64 474 us, 477; gradients of 64 ticks of them 636, 643.)
+// (To look costs 1 % of the time: 128 ticks of 20480 heads of 64 474 us, 477; gradients of 64 ticks of them 636, 646.)
 constexpr float kMostScale = 0x1p16f, kLargeState = 0x1p70f;
 constexpr int kSmallChunks = 64;
 
@@ -1022,8 +1022,7 @@ __global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tab
             turn ^= 1;
             if (threadIdx.x == 0) wild[turn] = again<Args>().exactly;
             lds_meet();
-            uint32_t odd = A::store(k, kr) | A::store(q, qr) | A::store(g, gr);
-            A::store(v, vr);
+            uint32_t odd = A::store(k, kr) | A::store(v, vr) | A::store(q, qr) | A::store(g, gr);
             if (small == 0) odd |= (uint32_t)A::large(turned) | (uint32_t)A::large(state);
             if (__ballot(odd != 0) && lane == 0) wild[turn] = 1;
             const uint64_t begins = __ballot(flag != 0);

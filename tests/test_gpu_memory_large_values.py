@@ -31,6 +31,18 @@ def values(d, dtype):
     d["v"][25, 0, 0] *= 1e-3
 
 
+def values_alone(d, dtype):
+    """v grad_out is beyond 32 bits where v alone is large, in ticks of their own."""
+    d["k"][:, 0, 0] *= 1e-9
+    d["q"][:, 0, 0] *= 1e-9
+    d["state"] *= 1e-9
+    d["grad_state"] *= 1e-9
+    d["grad_out"][:, 0, 0] *= 1e8
+    d["v"][5, 0, 0] *= 1e31 if dtype is F32 else 1e30
+    d["k"][5, 0, 0] *= 1e-30
+    d["log_decay"][0] = 0.0
+
+
 def gradients(d, dtype):
     for n in ("q", "v", "k", "state"):
         d[n] *= 1e-4
@@ -97,7 +109,7 @@ def cancelled(d, dtype):
         (d[n] if n == "grad_state" else d[n][:, 0, 0]).mul_(1e-14)
 
 
-PLANTS = [queries, values, gradients, scores, scores_of_values, state, faded, scale, cancelled]
+PLANTS = [queries, values, values_alone, gradients, scores, scores_of_values, state, faded, scale, cancelled]
 # (f16 ends where all of this begins: its states only, whatever they hold)
 CASES = [(p, t) for p in PLANTS for t in (F32, BF16)] + [(state, F16)]
 
