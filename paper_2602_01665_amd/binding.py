@@ -941,17 +941,26 @@ class TabxEnv:
         tabx_sample_levels(scores, sampling, uniform, self.st["next_level"], level_mask, env_mask,
                            stream)
 
+    def _fits(self, what, t, name):
+        """Heads of other rows than the batch's units would take the ticks and places of others (any whole number
+        of batches divides into them)."""
+        rows = t.shape[:-2].numel() if t.dim() > 2 else 0
+        if rows != self.E * self.N:
+            _refuse(what, f"{name} has {rows} rows of heads, not {self.E} x {self.N}")
+
     def rotate(self, x, pairs, frequency, y, interleaved=False, inverse=False, controlled=None, stream=None):
         """y = x [E, N, heads, width] turned by the tick of each env's episode and the place of each unit as the
         last tick left them: pairs of (t, x, y), frequency of all of them together."""
         axes = [(self.st[name], n) for name, n in zip(("t", "x", "y"), pairs)]
         if len(pairs) != 3:
             _refuse("rotate", f"pairs of {len(pairs)} axes, not of t, x and y")
+        self._fits("rotate", x, "x")
         tabx_rotary(x, axes, frequency, y, interleaved, inverse, controlled, stream)
 
     def remember(self, q, k, v, log_decay, scale, state, out, controlled=None, stream=None):
         """One tick of the units' memory, state [E, N, heads, key, value]: forgotten where the last tick ended an
         episode (`dones`).  After a reset of other envs the caller clears their states."""
+        self._fits("remember", q, "q")
         tabx_linear_attention_step(q, k, v, log_decay, scale, state, out, self.dones, controlled, stream)
 
     def snapshot(self) -> dict:

@@ -220,3 +220,27 @@ def test_a_batch_refuses_turns_of_other_axes(B):
             batch.remember(q, q, q, torch.zeros(2), 1.0, s, q)
         with pytest.raises(B.TabxError, match="state has"):
             batch.remember(q, q, q, torch.zeros(2), 1.0, s[:3], q)
+
+
+def test_a_batch_refuses_heads_of_other_rows(B):
+    """Ticks, places and ended episodes would be dealt out to them as if they were fewer, larger envs."""
+    from paper_2602_01665_amd import inputs as I
+    w = I.WORKLOADS["c2_4096env_5v5"]
+    env = B.TabxEnv(I.make_params(w, 4), I.make_scenario(w, 4), device="cpu")
+    freq, decay = torch.ones(6, dtype=torch.float64), torch.zeros(2)
+    for batch in [env] + env.parts(2):
+        E, N = batch.E, env.N
+        for lead in ((2 * E, N), (E, 2 * N), (3 * E * N,), (E, N, 2), (1, E * N + E)):
+            x, s = torch.zeros(*lead, 2, 12), torch.zeros(*lead, 2, 12, 12)
+            with pytest.raises(B.TabxError, match=f"rotate.*rows of heads, not {E} x {N}"):
+                batch.rotate(x, (2, 2, 2), freq, x)
+            with pytest.raises(B.TabxError, match=f"remember.*rows of heads, not {E} x {N}"):
+                batch.remember(x, x, x, decay, 1.0, s, x)
+        for lead in ((E, N), (E * N,)):
+            x, s = torch.zeros(*lead, 2, 12), torch.zeros(*lead, 2, 12, 12)
+            with pytest.raises(B.TabxError, match="not on a GPU"):
+                batch.rotate(x, (2, 2, 2), freq, x)
+            with pytest.raises(B.TabxError, match="not on a GPU"):
+                batch.remember(x, x, x, decay, 1.0, s, x)
+        with pytest.raises(B.TabxError, match="rows of heads"):
+            batch.rotate(torch.zeros(12), (2, 2, 2), freq, torch.zeros(12))
