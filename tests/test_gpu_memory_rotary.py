@@ -127,3 +127,35 @@ def test_many_rows(B):
         z = torch.empty_like(x[c])
         B.tabx_rotary(x[c], [(t[c], 4)], frequency, z)
         assert torch.equal(y[c], z)
+
+
+def test_more_rows_than_a_launch_has_workgroups(B):
+    """Rows of which a workgroup takes one at a time, and some of them a second: the same bits as rows alone."""
+    R, H, W = 2 ** 20 + 37, 1024, 2
+    g = torch.Generator("cuda").manual_seed(8)
+    x = torch.randn(1, H, W, generator=g, device="cuda").to(torch.bfloat16).expand(R, H, W)
+    t = torch.randint(0, 500, (R,), generator=g, device="cuda").to(torch.int32)
+    frequency = torch.tensor([0.7], dtype=torch.float64, device="cuda")
+    y = torch.empty(R, H, W, dtype=torch.bfloat16, device="cuda")
+    B.tabx_rotary(x, [(t, 1)], frequency, y)
+    for at in (0, 2 ** 19, 2 ** 20 - 3, R - 5):
+        c = slice(at, at + 5)
+        z = torch.empty(5, H, W, dtype=torch.bfloat16, device="cuda")
+        B.tabx_rotary(x[c], [(t[c], 1)], frequency, z)
+        assert torch.equal(y[c], z), at
+    M.near(z, *M.rotary(x[c].cpu(), [(t[c].cpu(), 1)], frequency.cpu(), False, False), "last ones")
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_rows_far_apart(B, dtype, interleaved):
+    """Rows, and heads, whose distances pass 32 bits inside a workgroup."""
+    R, H, W = 5, 3, 24
+    x, axes, frequency = make(9, R, H, W, (4, 5), dtype)
+    want = M.rotary(x, axes, frequency, interleaved, False)
+    far = torch.empty(2 ** 32 + 2 ** 20, dtype=dtype, device="cuda")
+    rows_far = far.as_strided((R, H, W), (2 ** 30 - 5, W + 1, 1), 7)
+    heads_far = far.as_strided((R, H, W), (W + 3, 2 ** 31 - 3, 1), 2 ** 14)
+    for view in (rows_far, heads_far):
+        M.near(run(B, x, axes, frequency, interleaved, False, y=view), *want, "output")
+        M.near(run(B, view, axes, frequency, interleaved, True), *M.rotary(view.cpu(), axes, frequency, interleaved, True), "input")
