@@ -194,3 +194,42 @@ def test_other_rows_are_as_they_were(B, plant, K, V, dtype):
         assert torch.equal(x.index_select(k, torch.arange(0, R, 2, device="cuda")), a.unsqueeze(k).expand_as(x.index_select(k, torch.arange(0, R, 2, device="cuda")))), n
         assert torch.equal(b, plain[n].select(k, 1)), n
         M.near(torch.stack((a, b), k), *want[n], n)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=str)
+@pytest.mark.parametrize("T,K,V", [(40, 128, 128), (130, 64, 64), (130, 96, 96), (2100, 16, 16)])
+def test_products_of_matrices_up_to_their_limits(B, T, K, V, dtype):
+    """All elements just below 2^30, a scale of 2^16, a state of nearly 2^70 that grows beyond it: the largest sums there
+    are before a chunk goes tick by tick, all of one sign."""
+    d = make(T, 1, 2, K, V, dtype)
+    for n in ("q", "k", "v", "grad_out"):
+        d[n] = torch.full_like(d[n], 2.0 ** 30 - 2.0 ** 22)
+    d["state"], d["grad_state"] = torch.full_like(d["state"], 2.0 ** 70 - 2.0 ** 60), torch.full_like(d["grad_state"], 2.0 ** 70 - 2.0 ** 60)
+    d["fresh"][:], d["log_decay"], d["scale"] = 0, torch.tensor([0.0, -1e-4]), 2.0 ** 16
+    want = expected(d)
+    for n, (value, _) in want.items():
+        assert 2.0 ** 60 < float(value.abs().max()) < 2.0 ** 127, n
+    for n, x in run(B, d).items():
+        M.near(x, *want[n], n)
+
+
+@pytest.mark.parametrize("grows", [False, True])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=str)
+def test_rows_of_more_chunks_than_a_state_is_trusted_for(B, dtype, grows):
+    """More than 64 chunks of one workgroup: a state that stays small, and one that has grown past 2^70 by then."""
+    T, R, K, V = 2200, 1100, 8, 8
+    assert B.tabx_linear_attention_workspace(T, R, 1, K, V) == 0
+    d = make(T, 1, 1, K, V, dtype)
+    d["log_decay"] = torch.zeros(1)
+    if grows:
+        for n in ("q", "k", "v", "grad_out"):
+            d[n] = torch.full_like(d[n], 2.0 ** 30 - 2.0 ** 22)
+        d["fresh"][:] = 0
+    want = expected(d)
+    assert (float(want["state_out"][0].abs().max()) > 2.0 ** 70) == grows
+    got = run(B, {n: x.expand(R, *x.shape[1:]).contiguous() if "state" in n else x.expand(T, R, *x.shape[2:]).contiguous()
+                  if isinstance(x, torch.Tensor) and n != "log_decay" else x for n, x in d.items()})
+    for n, x in got.items():
+        one = x.narrow(0 if "state" in n else 1, 0, 1)
+        assert torch.equal(x, one.expand_as(x)), n
+        M.near(one, *want[n], n)
