@@ -95,7 +95,7 @@ struct StepArgs {
 
 // A state is a run of keys x values floats.  LANES lanes have a row's head (64: a whole wavefront); lane l has four
 // consecutive values of every (4 LANES / VALUES)-th line of the state, so that the lanes read and write 16 bytes each of
-// one run.  Bound by HBM: the state is read (where it is not forgotten) and written, once each; 1310720 heads of 32 x 32
+// one run.  Bound by HBM: the state is read (also where it is forgotten) and written, once each; 1310720 heads of 32 x 32
 // 2.12 ms, 5.1 TB/s; 160000 of 80 x 48 964 us; 96 rows of 4 heads 4.5 us, with the launch 10.8.  Eight lines under way in
 // a lane at a time.  VALUES: the values, a multiple of four, rounded up to a power of two; lanes beyond the last value idle.
 template <int TYPE, int VALUES, int LANES>
@@ -198,7 +198,7 @@ __global__ __launch_bounds__(256) void tabx_attention_step_odd_kernel(const Step
 // state that is read) for f16 and f32, and of the parts' products those are left out that are below 2^-24 of a term.  For
 // bf16 it is cut into two, which round it to 16 bits: 2^-17 of a term, where the output's own rounding is 2^-8 of the result.
 // (A third one there: 128 ticks of 20480 heads of 64 502 us instead of 476, 64 ticks of 20480 heads of 96 844 instead of 622,
-// gradients of 64 ticks of 20480 heads of 64 719 instead of 639, of 5120 heads of 128 860 instead of 750.  For f16, whose
+// gradients of 64 ticks of 20480 heads of 64 719, in chunks of 32, instead of 639, of 5120 heads of 128 860 instead of 750.  For f16, whose
 // rounding is 2^-11, two and without the product of two second parts: 128 ticks of 20480 heads of 64 519 instead of 570.)
 template <int TYPE> struct Parts {
     static constexpr int in = TYPE == TABX_BF16 ? 1 : TYPE == TABX_F16 ? 2 : 3;
@@ -211,11 +211,11 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // Ticks of a chunk.  The state costs as many products a chunk, whatever its length; the ticks among themselves as many as they
 // are long, and longer ones more room.  With 64 and 32 of them, one part each (bf16):
-//   gradients, 64 ticks of 20480 heads of 64, 633 and 675 us; 64 ticks of 5120 heads of 128, 750 and 838;
-//     128 ticks of 40960 heads of 32, 1390 and 1009;
-//   forward, 128 ticks of 20480 heads of 64, 489 and 474; 64 ticks of 20480 heads of 96, 619 and 645; 32768 ticks of 8
-//     heads of 128, 152 and 165; 128 ticks of 81920 heads of 32, 1005 and 925;
-//   segments' states, 8192 ticks of 16 heads of 64, 47.5 and 48.7 with the attention behind them.
+//   gradients, 64 ticks of 20480 heads of 64, 643 and 685 us; 64 ticks of 5120 heads of 128, 746 and 859;
+//     128 ticks of 40960 heads of 32, 1409 and 1016;
+//   forward, 128 ticks of 20480 heads of 64, 493 and 475; 64 ticks of 20480 heads of 96, 627 and 654; 32768 ticks of 8
+//     heads of 128, 156 and 175; 128 ticks of 81920 heads of 32, 1005 and 908;
+//   segments' states, 8192 ticks of 16 heads of 64, 49.8 and 50.4 with the attention behind them.
 // Operands in several parts have no room for 64.  READS_ONCE: forward.
 constexpr int long_chunk(int d, int type, bool reads_once) { return type == TABX_BF16 && d > (reads_once ? 64 : 32) ? 64 : 32; }
 
@@ -760,8 +760,8 @@ struct Attention {
     };
 
     // One attention from tick `begin` to `last`; the next chunk's rows are under way while it works on the present one (not
-    // the wide ones', which have no registers left for them: 128 ticks of 10240 heads of 128 in bf16 2780 us with them, 650
-    // without; of 20480 heads of 64, 489 and 530).  READS: queries are answered (else only the state goes on).  part(),
+    // the wide ones', which have no registers left for them: 128 ticks of 10240 heads of 128 in bf16 1786 us with them, 653
+    // without; of 20480 heads of 64, 475 and 483).  READS: queries are answered (else only the state goes on).  part(),
     // course(begin): what to go through, worked out anew where it is needed.  kept: what is left of the state before.  wild, turn: of the chunk at hand and the one
     // before, whether it goes tick by tick.
     template <bool READS, typename GetPart, typename GetCourse>
@@ -869,9 +869,10 @@ __device__ __forceinline__ const Args &again()
 }
 
 // A workgroup goes through its ticks with the state in registers.  Bound by HBM and by vector instructions next to it, which
-// cut operands into parts and fade them: 128 ticks of 20480 heads of 64 in bf16 461 to 474 us, 4.3 TB/s of q, k, v and out
-// (vector instructions a half of the time, matrix ones a seventh, reads of LDS a third); of 10240 heads of 128 650 us (4.1);
-// in f32 128 ticks of 10240 heads of 64 392 (4.3); 8 ticks of 163840 heads of 64 1158 us (the states: 5.2).  CARRY: nothing is read, the states that the segments
+// cut operands into parts and fade them: 128 ticks of 20480 heads of 64 in bf16 455 to 475 us, 4.3 TB/s of q, k, v and out
+// (vector instructions two thirds of the time, matrix ones an eighth, reads of LDS a quarter); in f16, with its two parts, 556; of
+// 10240 heads of 128 653 us (4.1); in f32 128 ticks of 10240 heads of 64 388 (4.3); 8 ticks of 163840 heads of 64 1165 us (the
+// states: 5.2).  CARRY: nothing is read, the states that the segments
 // would leave of nothing are.
 template <int D, int TYPE, int C, bool CARRY>
 __global__ __launch_bounds__(4 * D, attention_wavefronts(D, TYPE)) void tabx_attention_kernel(const AttentionPair)
@@ -923,7 +924,7 @@ __global__ __launch_bounds__(4 * D, attention_wavefronts(D, TYPE)) void tabx_att
 
 // The gradients: forwards through the ticks for grad_q, then backwards for grad_k and grad_v, which read the same rows,
 // and the state's; the last chunk forwards is the first one backwards, and what was read is still in the caches.  Bound by
-// vector instructions (half of the time) beside HBM: 64 ticks of 20480 heads of 64 in bf16 634 us, 3.4 TB/s of seven arrays.
+// vector instructions (over half of the time) beside HBM: 64 ticks of 20480 heads of 64 in bf16 643 us, 3.4 TB/s of seven arrays.
 // The loads of the next chunk do not go ahead here: four arrays of rows would cost a wavefront of a SIMD.
 template <int D, int TYPE, int C>
 __global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tabx_attention_grad_kernel(const AttentionGradArgs)
@@ -1053,7 +1054,7 @@ __global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tab
 }
 
 // The gradients, each by a workgroup of its own: neighbours, which share what they read.  64 ticks of 5120 heads of 128 in
-// bf16 740 us; 100 ticks of 1887 heads of 48 x 80 in f32, half of them controlled, 372 us, most of it waits of one
+// bf16 746 us; 100 ticks of 1887 heads of 48 x 80 in f32, half of them controlled, 379 us, most of it waits of one
 // workgroup at a time on a CU for its own steps.
 template <int D, int TYPE, int C>
 __global__ __launch_bounds__(4 * D, attention_grad_wavefronts(D, TYPE)) void tabx_attention_grad_apart_kernel(const AttentionGradArgs)

@@ -231,9 +231,9 @@ static int form_width(int32_t keys, int32_t values)
 }
 
 // Into how many segments of how many ticks a row's ticks are cut: where there are few rows and heads, so many that every
-// CU has the workgroups that it holds, each of some chunks.  At least 64 ticks: 1024 ticks of 8 heads of 64 take 20 us,
-// their gradients 31; with 128 at least 25 and 43, with 256 36 and 69.  Half as many workgroups: 32768 ticks of 8 heads of
-// 128 190 us instead of 152, gradients of 512 ticks of 80 heads of 64 59 instead of 53 (of 8192 ticks of 16, 96 instead of 103).
+// CU has the workgroups that it holds, each of some chunks.  At least 64 ticks: 1024 ticks of 8 heads of 64 take 21 us,
+// their gradients 32; with 128 at least 27 and 44, with 256 40 and 71.  Half as many workgroups: 32768 ticks of 8 heads of
+// 128 197 us instead of 158, gradients of 512 ticks of 80 heads of 64 60 instead of 54 (of 8192 ticks of 16, 98 instead of 106).
 struct Segments {
     int64_t count, ticks;
 };
@@ -274,7 +274,7 @@ static int launch_attention_of(const AttentionPair &pair, int count, void *strea
     constexpr int chunk = long_chunk(D, TYPE, !CARRY);
     const int64_t groups = least(pair.of[0].works, kMostGroups);
     if constexpr (chunk > 32 && !CARRY)            // (no segments are that short)
-        // (8 ticks of 163840 heads of 64 were 1665 us in a chunk of 64, half empty, and are 1158)
+        // (8 ticks of 81920 heads of 96 1590 us, 1720 in a chunk of 64, half empty; of 128 2177 and 2142, 16 of 40960 1204 and 1197)
         if (pair.of[0].ticks <= 32) return launch_pair(tabx_attention_kernel<D, TYPE, 32, CARRY>, groups, 4 * D, pair, count, stream);
     return launch_pair(tabx_attention_kernel<D, TYPE, chunk, CARRY>, groups, 4 * D, pair, count, stream);
 }
@@ -311,9 +311,9 @@ static int carry(AttentionPair &pair, int count, int type, void *workspace, int6
 }
 
 // 16-bit operands of up to 64: one workgroup for all three gradients, which reads everything once where three would twice
-// (64 ticks of 20480 heads of 64 634 us, 760 apart; 128 ticks of 40960 heads of 32 1009 and 1093).  Wider or in three parts its
-// two states and four tiles cost more workgroups of a CU than they spare (64 ticks of 5120 heads of 128 957 us, 740 apart; f32,
-// 10240 heads of 64, 639 and 573).
+// (64 ticks of 20480 heads of 64 675 us, 783 apart; 128 ticks of 40960 heads of 32 1021 and 1114).  Wider or in three parts its
+// two states and four tiles cost more workgroups of a CU than they spare (64 ticks of 5120 heads of 128 967 us, 775 apart, of 10240
+// of 96 876 and 774; f32, 10240 heads of 64, 663 and 594; but 1887 of 48 x 80 353 and 380, where one workgroup runs either way).
 template <int D, int TYPE, int C>
 static int launch_attention_grad_of(const AttentionGradArgs &a, void *stream)
 {
@@ -336,7 +336,7 @@ static int launch_attention_grad_of(const AttentionGradArgs &a, void *stream)
 template <int D, int TYPE>
 static int launch_attention_grad(const AttentionGradArgs &a, void *stream)
 {
-    // of up to 32 ticks, half of a longer chunk would be empty (16 ticks of 81920 heads of 64: 1529 us, 1817 in one of 64)
+    // of up to 32 ticks, half of a longer chunk would be empty (16 ticks of 81920 heads of 64: 1542 us, 1756 in one of 64; 20480 of 128 1242 and 1308)
     constexpr int chunk = long_chunk(D, TYPE, false);
     if constexpr (chunk > 32)
         if (a.ticks <= 32) return launch_attention_grad_of<D, TYPE, 32>(a, stream);
